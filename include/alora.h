@@ -204,7 +204,7 @@ alora_status alora_set_option(alora_ctx *ctx, const char *key, int value);
  * with HIP events on the call's stream.  alora_profile_read waits for the pending events and
  * returns the accumulated time and launch count of one kernel family: "prep_rows",
  * "qkv_gemm", "rope_append", "attn_prefill", "attn_decode", "attn_merge", "o_proj",
- * "mlp_norm", "gate_up", "silu_mul", "down_proj", "lm_head", "lm_argmax".  alora_profile_reset
+ * "mlp_norm", "gate_up", "silu_mul", "down_proj", "lm_head", "lm_argmax", "row_move".  alora_profile_reset
  * clears the totals. */
 alora_status alora_profile_read(alora_ctx *ctx, const char *kernel, double *total_ms, int64_t *launches);
 alora_status alora_profile_reset(alora_ctx *ctx);
@@ -305,6 +305,88 @@ alora_status alora_stack_decode(alora_ctx *ctx, const alora_layer_desc *layers, 
 alora_status alora_lm_head(alora_ctx *ctx, alora_dtype dtype, int32_t d, int32_t vocab, const void *x_last,
                            const void *final_gain, float rms_eps, const void *W_vocab, int32_t B,
                            float *logits, int32_t *token, void *stream);
+
+/* ---- Rows of a cache: copying them, and holding them in 4 bits -----------------------------------------------
+ *
+ * A context that waits for its next adapter (Section 2, "Cache reuse patterns") need not stay in the storage type.  An
+ * alora_qcache holds the same rows in 4 bits and 1/32 byte per channel -- 3.76 times less than bf16, 7.5 times less than fp32 --
+ * and the calls below read and write it: rows go in and out (alora_qcache_store / _load), are copied like those of an
+ * alora_kv_cache (alora_qcache_copy, alora_cache_copy), and prefill, decode and plain attention run over them
+ * (alora_qcache_prefill, ..., alora_qcache_attend).
+ *
+ * Format.  Row (token, kv head) has head_dim codes of 4 bits: a sign (bit 3) and a magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits
+ * 2..0 = 0..7); element 2i is in the low half of byte i.  Each 32 channels of a head (the last block may be shorter) share one
+ * exponent byte E: value = code * 2^(E - 127).  Storing takes E - 127 = e - 2 from the block's largest magnitude m * 2^e, 1 <= m < 2, or
+ * e - 1 where m > 1.75 (at most a seventh of that magnitude is cut off), kept between -125 and 125, and rounds every channel to the
+ * nearest code, ties to the even one, magnitudes over 6 to 6.  Scales are powers of two, so a code depends on nothing but its
+ * block's bits, and loading is exact in bf16 and fp32.  A block that holds a NaN or an infinity gets E = 255: all its values are NaN.
+ * Other E outside [2, 252] are never stored; what attention makes of them is undefined. */
+typedef struct {
+  void *k;                     /* DEVICE [pool_tokens, n_kv_heads, head_dim / 2] codes  */
+  void *v;                     /* DEVICE, same shape                                    */
+  void *k_scale;               /* DEVICE [pool_tokens, n_kv_heads, ceil(head_dim / 32)] exponent bytes */
+  void *v_scale;               /* DEVICE, same shape                                    */
+  int64_t pool_tokens;
+  const int64_t *seq_offset;   /* HOST, these and below as in alora_kv_cache            */
+  const int32_t *seq_capacity;
+  int32_t *seq_len;
+  const int64_t *prefix_offset;
+  const int32_t *prefix_len;
+} alora_qcache;
+
+/* n rows: source rows src .. src + n - 1 become destination rows dst .. dst + n - 1 (pool rows, whatever sequence they belong to). */
+typedef struct { int64_t src, dst, n; } alora_row_range;
+
+/* Copies rows inside one pool or from pool to pool, in n_layers layers at once: forking a context into rows that a sequence may
+ * write behind, closing a pool up after sequences have ended, moving a sequence to a larger region.  The result is as if every source
+ * row had been read before any destination row was written, so ranges may move rows over each other (dst[l] and src[l] the same
+ * arrays).  The bookkeeping -- whose rows they are now -- is the caller's: only k, v and pool_tokens of the caches are read.
+ *   dst, src  HOST [n_layers]: caches of one shape (dtype, n_kv_heads, head_dim); pools may differ in size, each is the same in all layers
+ *   ranges    HOST [n_ranges]; rows outside a pool: ALORA_ECAPACITY; destination ranges that overlap each other, negative n: ALORA_EINVAL.
+ *             n = 0 is allowed, and n_ranges = 0 is a valid no-op.
+ * dst[l] and src[l] are the same arrays or do not overlap in memory (ALORA_EINVAL where bases differ and memory overlaps).  Rows that move
+ * over others, in more than one order, are staged through the context's workspace. */
+alora_status alora_cache_copy(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_kv_cache *dst,
+                              const alora_kv_cache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
+/* The same for rows of 4 bits: codes and exponents. */
+alora_status alora_qcache_copy(alora_ctx *ctx, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *dst, const alora_qcache *src,
+                               int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
+/* Rows of the storage type into rows of 4 bits, and back.  Ranges as above; dst and src never share memory.  All four calls with at most 16
+ * ranges and 32 layers (copies of 4 bits: 16) launch one kernel and nothing else, unless rows move over each other: such a call may be captured into a HIP graph.
+ * Under capture the others are refused (ALORA_EINVAL). */
+alora_status alora_qcache_store(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *dst,
+                                const alora_kv_cache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
+alora_status alora_qcache_load(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_kv_cache *dst,
+                               const alora_qcache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
+
+/* Attention of given queries over cached rows of 4 bits: the second half of alora_qcache_prefill / _decode by itself, for callers with
+ * projections of their own.  Nothing is written but out.
+ *   q          DEVICE [T, n_q_heads * head_dim] (dtype): rotated queries, sequences back to back
+ *   cu_seqlens HOST [B+1] as in alora_prefill.  The S_b rows of sequence b are the last S_b of its seq_len[b] cached positions, all of them in its own
+ *              rows (S_b <= seq_len[b] - prefix_len[b]): row i sees positions 0 .. seq_len[b] - S_b + i.  S_b = 0 leaves a sequence alone.
+ *   out        DEVICE [T, n_q_heads * head_dim] (dtype)
+ * softmax(q k / sqrt(head_dim)) v with queries, keys and values as they are (no rounding), sums in fp32.  A NaN in a key or value reaches the
+ * rows that see its position and no others.  Sequences of the call may name the same rows.  Prefixes that several sequences name are walked once for all of
+ * them.  Errors as everywhere; under capture into a HIP graph ALORA_EINVAL (the call stages its work list from the host). */
+alora_status alora_qcache_attend(alora_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *cache,
+                                 const void *q, const int32_t *cu_seqlens, int32_t B, void *out, void *stream);
+
+/* alora_prefill, alora_decode, alora_stack_prefill and alora_stack_decode on caches of 4 bits.  The new keys and values are computed
+ * as there (rounded to the storage type, rotated), stored in 4 bits behind the cached rows, and read back from there by the attention like every
+ * other row: a later call that reads the same rows sees the same numbers.  Everything else -- arguments, shared prefixes, order of
+ * validation, seq_len -- is as in the calls they are named after.  Rows before the invocation index come out with the same
+ * codes whatever call wrote them, as long as their keys and values do there.  Not under capture. */
+alora_status alora_qcache_prefill(alora_ctx *ctx, const alora_layer_desc *layer, alora_qcache *cache, const void *x_suffix,
+                                  const int32_t *cu_seqlens, const int32_t *k_per_seq, const int32_t *adapter_per_seq, int32_t B,
+                                  void *attn_out, void *stream);
+alora_status alora_qcache_decode(alora_ctx *ctx, const alora_layer_desc *layer, alora_qcache *cache, const void *x_tok,
+                                 const int32_t *k_per_seq, const int32_t *adapter_per_seq, int32_t B, void *attn_out, void *stream);
+alora_status alora_qcache_stack_prefill(alora_ctx *ctx, const alora_layer_desc *layers, int32_t n_layers, alora_qcache *caches,
+                                        const void *x, const int32_t *cu_seqlens, const int32_t *k_per_seq,
+                                        const int32_t *adapter_per_seq, int32_t B, void *out, void *stream);
+alora_status alora_qcache_stack_decode(alora_ctx *ctx, const alora_layer_desc *layers, int32_t n_layers, alora_qcache *caches,
+                                       const void *x_tok, const int32_t *k_per_seq, const int32_t *adapter_per_seq, int32_t B,
+                                       void *out, void *stream);
 
 #ifdef __cplusplus
 }

@@ -18,9 +18,12 @@ ALORA_OK, ALORA_EINVAL, ALORA_ESHAPE, ALORA_ECAPACITY, ALORA_EADAPTER, ALORA_EDT
 ALORA_F32, ALORA_BF16 = 0, 1
 
 EXPORTS = ["alora_create", "alora_destroy", "alora_last_error", "alora_status_string", "alora_set_option",
-           "alora_profile_read", "alora_profile_reset", "alora_prefill", "alora_decode", "alora_decode_static", "alora_decode_steps", "alora_stack_prefill", "alora_stack_decode", "alora_lm_head"]
+           "alora_profile_read", "alora_profile_reset", "alora_prefill", "alora_decode", "alora_decode_static", "alora_decode_steps", "alora_stack_prefill", "alora_stack_decode", "alora_lm_head",
+           "alora_cache_copy", "alora_qcache_copy", "alora_qcache_store", "alora_qcache_load", "alora_qcache_attend", "alora_qcache_prefill",
+           "alora_qcache_decode", "alora_qcache_stack_prefill", "alora_qcache_stack_decode"]
 KERNELS = ["lm_head", "lm_argmax", "prep_rows", "qkv_gemm", "rope_append", "attn_prefill", "attn_decode", "attn_merge", "o_proj",
-           "mlp_norm", "gate_up", "silu_mul", "down_proj"]
+           "mlp_norm", "gate_up", "silu_mul", "down_proj", "row_move"]
+Q_BLOCK = 32                 # channels of a row of 4 bits that share an exponent
 
 
 class LayerDesc(C.Structure):
@@ -40,6 +43,16 @@ class KVCacheDesc(C.Structure):
                 ("seq_offset", C.POINTER(C.c_int64)), ("seq_capacity", C.POINTER(C.c_int32)),
                 ("seq_len", C.POINTER(C.c_int32)),
                 ("prefix_offset", C.POINTER(C.c_int64)), ("prefix_len", C.POINTER(C.c_int32))]
+
+
+class QCacheDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("pool_tokens", C.c_int64),
+                ("seq_offset", C.POINTER(C.c_int64)), ("seq_capacity", C.POINTER(C.c_int32)), ("seq_len", C.POINTER(C.c_int32)),
+                ("prefix_offset", C.POINTER(C.c_int64)), ("prefix_len", C.POINTER(C.c_int32))]
+
+
+class RowRange(C.Structure):
+    _fields_ = [("src", C.c_int64), ("dst", C.c_int64), ("n", C.c_int64)]
 
 
 def load_library() -> C.CDLL:
@@ -82,6 +95,19 @@ def load_library() -> C.CDLL:
     lib.alora_stack_decode.restype = C.c_int
     lib.alora_stack_decode.argtypes = [C.c_void_p, C.POINTER(LayerDesc), C.c_int32, C.POINTER(KVCacheDesc), C.c_void_p,
                                        C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32, C.c_void_p, C.c_void_p]
+    i32, kvp, qp, rp, vp = C.c_int32, C.POINTER(KVCacheDesc), C.POINTER(QCacheDesc), C.POINTER(RowRange), C.c_void_p
+    lib.alora_cache_copy.argtypes = [vp, i32, i32, i32, kvp, kvp, i32, rp, i32, vp]
+    lib.alora_qcache_copy.argtypes = [vp, i32, i32, qp, qp, i32, rp, i32, vp]
+    lib.alora_qcache_store.argtypes = [vp, i32, i32, i32, qp, kvp, i32, rp, i32, vp]
+    lib.alora_qcache_load.argtypes = [vp, i32, i32, i32, kvp, qp, i32, rp, i32, vp]
+    lib.alora_qcache_attend.argtypes = [vp, i32, i32, i32, i32, qp, vp, i32p, i32, vp, vp]
+    lib.alora_qcache_prefill.argtypes = [vp, C.POINTER(LayerDesc), qp, vp, i32p, i32p, i32p, i32, vp, vp]
+    lib.alora_qcache_decode.argtypes = [vp, C.POINTER(LayerDesc), qp, vp, i32p, i32p, i32, vp, vp]
+    lib.alora_qcache_stack_prefill.argtypes = [vp, C.POINTER(LayerDesc), i32, qp, vp, i32p, i32p, i32p, i32, vp, vp]
+    lib.alora_qcache_stack_decode.argtypes = [vp, C.POINTER(LayerDesc), i32, qp, vp, i32p, i32p, i32, vp, vp]
+    for name in ("cache_copy", "qcache_copy", "qcache_store", "qcache_load", "qcache_attend", "qcache_prefill", "qcache_decode",
+                 "qcache_stack_prefill", "qcache_stack_decode"):
+        getattr(lib, "alora_" + name).restype = C.c_int
     return lib
 
 
@@ -132,12 +158,14 @@ class Layer:
         self.device = W.device
 
 
-class KVCache:
-    """A flat pool of token rows [pool_tokens, n_kv_heads, head_dim] for keys and for values, plus the
-    host-side table that says which rows belong to which sequence and how many are valid."""
+def _table(x, dtype):
+    return None if x is None else np.ascontiguousarray(np.asarray(x, dtype=dtype))
 
-    def __init__(self, capacities: Sequence[int], n_kv_heads: int, head_dim: int, dtype: torch.dtype, device,
-                 fill: Optional[float] = None, guard_rows: int = 0):
+
+class _Pool:
+    """The host-side table of a pool of token rows: which rows belong to which sequence, and how many are valid."""
+
+    def _regions(self, capacities: Sequence[int], guard_rows: int):
         caps = [int(c) for c in capacities]
         self.seq_capacity = _i32(caps)
         offs, o = [], guard_rows
@@ -149,22 +177,21 @@ class KVCache:
         self.seq_len = np.zeros(len(caps), dtype=np.int32)
         self.prefix_offset = None        # set by share_prefix
         self.prefix_len = None
-        shape = (self.pool_tokens, n_kv_heads, head_dim)
-        if fill is None:
-            self.k = torch.zeros(shape, dtype=dtype, device=device)
-            self.v = torch.zeros(shape, dtype=dtype, device=device)
-        else:
-            self.k = torch.full(shape, fill, dtype=dtype, device=device)
-            self.v = torch.full(shape, -fill, dtype=dtype, device=device)
-        self._refresh()
 
-    def _refresh(self):
-        self.desc = KVCacheDesc(self.k.data_ptr(), self.v.data_ptr(), self.pool_tokens,
-                                self.seq_offset.ctypes.data_as(C.POINTER(C.c_int64)),
-                                self.seq_capacity.ctypes.data_as(C.POINTER(C.c_int32)),
-                                self.seq_len.ctypes.data_as(C.POINTER(C.c_int32)),
-                                None if self.prefix_len is None else self.prefix_offset.ctypes.data_as(C.POINTER(C.c_int64)),
-                                None if self.prefix_len is None else self.prefix_len.ctypes.data_as(C.POINTER(C.c_int32)))
+    def _wrap(self, pool_tokens, seq_offset, seq_capacity, seq_len, prefix_offset, prefix_len):
+        self.pool_tokens = int(pool_tokens)
+        self.seq_offset, self.seq_capacity = _table(seq_offset, np.int64), _table(seq_capacity, np.int32)
+        self.seq_len = _table(seq_len, np.int32)
+        self.prefix_offset, self.prefix_len = _table(prefix_offset, np.int64), _table(prefix_len, np.int32)
+        self._refresh()
+        return self
+
+    def _tables(self):
+        def of(a, t):
+            return None if a is None else a.ctypes.data_as(C.POINTER(t))
+        shared = self.prefix_len is not None
+        return (of(self.seq_offset, C.c_int64), of(self.seq_capacity, C.c_int32), of(self.seq_len, C.c_int32),
+                of(self.prefix_offset, C.c_int64) if shared else None, of(self.prefix_len, C.c_int32))
 
     def share_prefix(self, b: int, pool_row: int, n: int):
         """Positions 0..n-1 of sequence b are read from pool rows pool_row.. (one copy that several sequences
@@ -177,6 +204,35 @@ class KVCache:
         self.seq_len[b] = max(int(self.seq_len[b]), int(n))
         self._refresh()
 
+
+class KVCache(_Pool):
+    """A flat pool of token rows [pool_tokens, n_kv_heads, head_dim] for keys and for values, plus the
+    host-side table that says which rows belong to which sequence and how many are valid."""
+
+    def __init__(self, capacities: Sequence[int], n_kv_heads: int, head_dim: int, dtype: torch.dtype, device,
+                 fill: Optional[float] = None, guard_rows: int = 0):
+        self._regions(capacities, guard_rows)
+        shape = (self.pool_tokens, n_kv_heads, head_dim)
+        if fill is None:
+            self.k = torch.zeros(shape, dtype=dtype, device=device)
+            self.v = torch.zeros(shape, dtype=dtype, device=device)
+        else:
+            self.k = torch.full(shape, fill, dtype=dtype, device=device)
+            self.v = torch.full(shape, -fill, dtype=dtype, device=device)
+        self._refresh()
+
+    @classmethod
+    def from_tensors(cls, k: torch.Tensor, v: torch.Tensor, seq_offset=None, seq_capacity=None, seq_len=None, prefix_offset=None,
+                     prefix_len=None) -> "KVCache":
+        """A cache over tensors that exist, k and v [pool_tokens, n_kv_heads, head_dim]; the table only where a call needs it."""
+        assert k.shape == v.shape and k.dtype == v.dtype and k.dim() == 3, "k and v are of one shape and type"
+        self = cls.__new__(cls)
+        self.k, self.v = k, v
+        return self._wrap(k.shape[0], seq_offset, seq_capacity, seq_len, prefix_offset, prefix_len)
+
+    def _refresh(self):
+        self.desc = KVCacheDesc(_ptr(self.k), _ptr(self.v), self.pool_tokens, *self._tables())
+
     def rows(self, b: int, lo: int, hi: int):
         o = int(self.seq_offset[b])
         return self.k[o + lo:o + hi], self.v[o + lo:o + hi]
@@ -188,6 +244,35 @@ class KVCache:
         self.k[o:o + n] = K.to(self.k.dtype).view(n, *self.k.shape[1:]).to(self.k.device)
         self.v[o:o + n] = V.to(self.v.dtype).view(n, *self.v.shape[1:]).to(self.v.device)
         self.seq_len[b] = n
+
+
+class QCache(_Pool):
+    """A pool of token rows in 4 bits: codes [pool_tokens, n_kv_heads, head_dim / 2] and exponents
+    [pool_tokens, n_kv_heads, ceil(head_dim / 32)], uint8, for keys and for values, and the table of a KVCache."""
+
+    def __init__(self, capacities: Sequence[int], n_kv_heads: int, head_dim: int, device, guard_rows: int = 0):
+        self._regions(capacities, guard_rows)
+        self.head_dim = int(head_dim)
+        codes = (self.pool_tokens, n_kv_heads, head_dim // 2)
+        scales = (self.pool_tokens, n_kv_heads, (head_dim + Q_BLOCK - 1) // Q_BLOCK)
+        self.k, self.v = (torch.zeros(codes, dtype=torch.uint8, device=device) for _ in range(2))
+        self.k_scale, self.v_scale = (torch.full(scales, 127, dtype=torch.uint8, device=device) for _ in range(2))
+        self._refresh()
+
+    @classmethod
+    def from_tensors(cls, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, seq_offset=None,
+                     seq_capacity=None, seq_len=None, prefix_offset=None, prefix_len=None) -> "QCache":
+        """A cache over tensors that exist; the table only where a call needs it."""
+        h = 2 * int(k.shape[-1])
+        assert k.shape == v.shape and k_scale.shape == v_scale.shape == (*k.shape[:2], (h + Q_BLOCK - 1) // Q_BLOCK), "codes and exponents of one cache"
+        assert all(t.dtype == torch.uint8 for t in (k, v, k_scale, v_scale)), "codes and exponents are uint8"
+        self = cls.__new__(cls)
+        self.head_dim = h
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        return self._wrap(k.shape[0], seq_offset, seq_capacity, seq_len, prefix_offset, prefix_len)
+
+    def _refresh(self):
+        self.desc = QCacheDesc(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), self.pool_tokens, *self._tables())
 
 
 class Context:
@@ -345,3 +430,134 @@ def alora_stack_decode(ctx: Context, layers: List[Layer], caches: List[KVCache],
         if c.seq_len is not caches[0].seq_len:
             c.seq_len[:] = caches[0].seq_len
     return out
+
+
+# ---- rows of a cache: copying them, and holding them in 4 bits ---------------------------------------------------
+def _ranges(ranges) -> np.ndarray:
+    r = np.ascontiguousarray(np.asarray(ranges, dtype=np.int64).reshape(-1, 3))
+    return r
+
+
+def _caches(caches):
+    """One cache or a list of them (one per layer) -> the C array, the number, the first."""
+    if isinstance(caches, _Pool):
+        return C.byref(caches.desc), 1, caches
+    n = len(caches)
+    return (type(caches[0].desc) * n)(*[c.desc for c in caches]), n, caches[0]
+
+
+def _row_shape(kv: KVCache):
+    return {torch.float32: ALORA_F32, torch.bfloat16: ALORA_BF16}[kv.k.dtype], int(kv.k.shape[1]), int(kv.k.shape[2])
+
+
+def _same_shape(x, y, shape_of):
+    if shape_of(x) != shape_of(y):
+        raise ValueError(f"caches of different shapes: {shape_of(x)} and {shape_of(y)}")
+
+
+def _q_shape(c):
+    return (int(c.k.shape[1]), c.head_dim) if isinstance(c, QCache) else (int(c.k.shape[1]), int(c.k.shape[2]))
+
+
+def alora_cache_copy(ctx: Context, dst, src, ranges, stream=None):
+    """ranges [n, 3] of (source row, destination row, rows): pool rows of `src` to pool rows of `dst` (a KVCache, or a list of them, one per
+    layer), as if every row had been read before any is written; dst and src may be the same caches."""
+    d, n, d0 = _caches(dst)
+    s, m, s0 = _caches(src)
+    _same_shape(d0, s0, _row_shape)
+    if n != m:
+        raise ValueError(f"{n} destination and {m} source layers")
+    r = _ranges(ranges)
+    dt, heads, h = _row_shape(d0)
+    ctx._check(_lib.alora_cache_copy(ctx._h, dt, heads, h, d, s, n, r.ctypes.data_as(C.POINTER(RowRange)), len(r), _stream_ptr(stream)))
+
+
+def alora_qcache_copy(ctx: Context, dst, src, ranges, stream=None):
+    """alora_cache_copy for QCaches."""
+    d, n, d0 = _caches(dst)
+    s, m, s0 = _caches(src)
+    _same_shape(d0, s0, _q_shape)
+    if n != m:
+        raise ValueError(f"{n} destination and {m} source layers")
+    r = _ranges(ranges)
+    heads, h = _q_shape(d0)
+    ctx._check(_lib.alora_qcache_copy(ctx._h, heads, h, d, s, n, r.ctypes.data_as(C.POINTER(RowRange)), len(r), _stream_ptr(stream)))
+
+
+def alora_qcache_store(ctx: Context, dst, src, ranges, stream=None):
+    """Rows of KVCaches (src) into rows of 4 bits (dst): ranges as in alora_cache_copy."""
+    d, n, d0 = _caches(dst)
+    s, m, s0 = _caches(src)
+    _same_shape(d0, s0, _q_shape)
+    if n != m:
+        raise ValueError(f"{n} destination and {m} source layers")
+    r = _ranges(ranges)
+    ctx._check(_lib.alora_qcache_store(ctx._h, *_row_shape(s0), d, s, n, r.ctypes.data_as(C.POINTER(RowRange)), len(r), _stream_ptr(stream)))
+
+
+def alora_qcache_load(ctx: Context, dst, src, ranges, stream=None):
+    """Rows of 4 bits (src) into rows of KVCaches (dst), exactly."""
+    d, n, d0 = _caches(dst)
+    s, m, s0 = _caches(src)
+    _same_shape(d0, s0, _q_shape)
+    if n != m:
+        raise ValueError(f"{n} destination and {m} source layers")
+    r = _ranges(ranges)
+    ctx._check(_lib.alora_qcache_load(ctx._h, *_row_shape(d0), d, s, n, r.ctypes.data_as(C.POINTER(RowRange)), len(r), _stream_ptr(stream)))
+
+
+def alora_qcache_attend(ctx: Context, cache: QCache, q: torch.Tensor, cu_seqlens: Sequence[int], n_q_heads: int,
+                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q [T, n_q_heads * head_dim], rotated queries of the last rows of every sequence -> attention over the cache."""
+    cu = _i32(cu_seqlens)
+    heads, h = _q_shape(cache)
+    if out is None:
+        out = torch.empty_like(q)
+    if q.dim() != 2 or q.shape[1] != n_q_heads * h or q.shape[0] != int(cu[-1]) or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError(f"q {tuple(q.shape)} and out {tuple(out.shape)} have to be [{int(cu[-1])}, {n_q_heads * h}] of one type")
+    dt = {torch.float32: ALORA_F32, torch.bfloat16: ALORA_BF16}[q.dtype]
+    ctx._check(_lib.alora_qcache_attend(ctx._h, dt, n_q_heads, heads, h, C.byref(cache.desc), _ptr(q), cu.ctypes.data_as(C.POINTER(C.c_int32)),
+                                        len(cu) - 1, _ptr(out), _stream_ptr(stream)))
+    return out
+
+
+def _q_call(name, ctx, layers, caches, x, cu, k_per_seq, adapter_per_seq, out, width, stream):
+    """The four calls on QCaches that run layers; cu = None: one row per sequence; width: columns of the output."""
+    kk, ad = _i32(k_per_seq), _i32(adapter_per_seq)
+    stack = "stack" in name
+    if out is None:
+        out = torch.empty((x.shape[0], width), dtype=layers[0].dtype, device=layers[0].device)
+    p = C.POINTER(C.c_int32)
+    descs = (QCacheDesc * len(caches))(*[c.desc for c in caches])
+    args = [ctx._h, (LayerDesc * len(layers))(*[l.desc for l in layers])] + ([len(layers)] if stack else []) + [descs, _ptr(x)]
+    if cu is not None:
+        cu = _i32(cu)
+        args.append(cu.ctypes.data_as(p))
+    st = getattr(_lib, name)(*args, kk.ctypes.data_as(p), ad.ctypes.data_as(p), len(kk), _ptr(out), _stream_ptr(stream))
+    ctx._check(st)
+    # the library updated the seq_len array that caches[0] points at; mirror it to the others
+    for c in caches[1:]:
+        if c.seq_len is not caches[0].seq_len:
+            c.seq_len[:] = caches[0].seq_len
+    return out
+
+
+def alora_qcache_prefill(ctx: Context, layer: Layer, cache: QCache, x_suffix: torch.Tensor, cu_seqlens: Sequence[int], k_per_seq: Sequence[int],
+                         adapter_per_seq: Sequence[int], attn_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    return _q_call("alora_qcache_prefill", ctx, [layer], [cache], x_suffix, cu_seqlens, k_per_seq, adapter_per_seq, attn_out, layer.n_q, stream)
+
+
+def alora_qcache_decode(ctx: Context, layer: Layer, cache: QCache, x_tok: torch.Tensor, k_per_seq: Sequence[int],
+                        adapter_per_seq: Sequence[int], attn_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    return _q_call("alora_qcache_decode", ctx, [layer], [cache], x_tok, None, k_per_seq, adapter_per_seq, attn_out, layer.n_q, stream)
+
+
+def alora_qcache_stack_prefill(ctx: Context, layers: List[Layer], caches: List[QCache], x: torch.Tensor, cu_seqlens: Sequence[int],
+                               k_per_seq: Sequence[int], adapter_per_seq: Sequence[int], out: Optional[torch.Tensor] = None,
+                               stream=None) -> torch.Tensor:
+    return _q_call("alora_qcache_stack_prefill", ctx, layers, caches, x, cu_seqlens, k_per_seq, adapter_per_seq, out, layers[0].d, stream)
+
+
+def alora_qcache_stack_decode(ctx: Context, layers: List[Layer], caches: List[QCache], x_tok: torch.Tensor, k_per_seq: Sequence[int],
+                              adapter_per_seq: Sequence[int], out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    return _q_call("alora_qcache_stack_decode", ctx, layers, caches, x_tok, None, k_per_seq, adapter_per_seq, out, layers[0].d, stream)

@@ -13,6 +13,7 @@
 #include "../../include/alora.h"
 #include "common.h"
 #include "mfma_kernels.h"
+#include "qcache.h"
 
 using namespace alora;
 
@@ -81,9 +82,9 @@ struct ProfEvent {
 
 static const char *const KERNEL_NAMES[] = {"prep_rows", "qkv_gemm", "rope_append", "attn_prefill", "attn_decode",
                                            "attn_merge", "o_proj", "mlp_norm", "gate_up", "silu_mul", "down_proj",
-                                           "lm_head", "lm_argmax"};
+                                           "lm_head", "lm_argmax", "row_move"};
 enum KernelId { K_PREP = 0, K_QKV, K_ROPE, K_ATTN_PREFILL, K_ATTN_DECODE, K_ATTN_MERGE, K_OPROJ, K_MLPNORM,
-                K_GATEUP, K_SILU, K_DOWN, K_LMHEAD, K_ARGMAX, K_COUNT };
+                K_GATEUP, K_SILU, K_DOWN, K_LMHEAD, K_ARGMAX, K_ROWS, K_COUNT };
 
 struct alora_ctx {
   int opt_profile = 0;
@@ -294,7 +295,7 @@ alora_status check_layer(alora_ctx *ctx, const alora_layer_desc *ly, bool need_t
 }
 
 alora_status check_batch(alora_ctx *ctx, const alora_layer_desc *ly, const alora_kv_cache *cache,
-                         const int32_t *cu, const int32_t *kps, const int32_t *aps, int B, int n_steps, Plan *pl) {
+                         const int32_t *cu, const int32_t *kps, const int32_t *aps, int B, int n_steps, Plan *pl, bool writes = true) {
   if (!cache) return fail(ctx, ALORA_EINVAL, "cache is NULL");
   if (B < 1) return fail(ctx, ALORA_EINVAL, "B = %d must be at least 1", B);
   if (!cu || !kps || !aps) return fail(ctx, ALORA_EINVAL, "cu_seqlens / k_per_seq / adapter_per_seq is NULL");
@@ -358,8 +359,8 @@ alora_status check_batch(alora_ctx *ctx, const alora_layer_desc *ly, const alora
   pl->T = cu[B];
   count_adapted_tiles(pl, n_steps - 1);
   // The regions the sequences own must be disjoint, and nobody may write where somebody reads a shared prefix:
-  // the kernels would write those cache rows concurrently, silently.
-  {
+  // the kernels would write those cache rows concurrently, silently.  (Calls that only read may name rows twice.)
+  if (writes) {
     struct Iv { int64_t lo, hi; int b; };
     std::vector<Iv> own, wr, pf;
     for (int b = 0; b < B; ++b) {
@@ -1343,9 +1344,353 @@ double run_pass_us(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, con
          1.7 * (double)pl.T * L.n_q_heads * (pp.n_own + pp.n_sh + 1) * (2 * 520) / 4e6;
 }
 
+// The calls on rows.  No exception leaves them: what cannot be allocated on the host is an error like any other.
+template <typename F>
+alora_status guarded(alora_ctx *ctx, F f) {
+  if (!ctx) return ALORA_EINVAL;
+  try {
+    ctx->err.clear();
+    return f();
+  } catch (...) {
+    return fail(ctx, ALORA_EHIP, "out of host memory");
+  }
+}
+
+// ---- rows of a cache: moving them, rows of 4 bits (alora_cache_copy, alora_qcache_*) ----------------------------------------
+bool is_capturing(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) != hipSuccess) { (void)hipGetLastError(); return false; }
+  return st != hipStreamCaptureStatusNone;
+}
+
+alora_status check_row_shape(alora_ctx *ctx, int n_kv_heads, int head_dim, int n_layers, const void *dst, const void *src) {
+  if (n_kv_heads < 1 || n_kv_heads > 65536) return fail(ctx, ALORA_ESHAPE, "n_kv_heads = %d outside [1, 65536]", n_kv_heads);
+  if (head_dim < 2 || head_dim > 256 || (head_dim & 1)) return fail(ctx, ALORA_ESHAPE, "head_dim = %d must be even and in [2, 256]", head_dim);
+  if (n_layers < 1 || n_layers > 8192) return fail(ctx, ALORA_EINVAL, "n_layers = %d outside [1, 8192]", n_layers);
+  if (!dst || !src) return fail(ctx, ALORA_EINVAL, "dst / src is NULL");
+  return ALORA_OK;
+}
+
+// The ranges of a call, checked; those that leave rows where they are (in_place) and empty ones are dropped.
+struct RowJob {
+  std::vector<RowRange> ranges;
+  int64_t rows = 0;
+  bool over = false;      // in_place: some range writes rows that another one (or itself) reads
+};
+alora_status check_ranges(alora_ctx *ctx, const alora_row_range *r, int n, int64_t src_tokens, int64_t dst_tokens, bool in_place, RowJob *job) {
+  if (n < 0) return fail(ctx, ALORA_EINVAL, "n_ranges = %d is negative", n);
+  if (n > 0 && !r) return fail(ctx, ALORA_EINVAL, "ranges is NULL");
+  if (src_tokens < 0 || dst_tokens < 0) return fail(ctx, ALORA_ECAPACITY, "pool_tokens is negative");
+  std::vector<RowRange> by_dst;
+  job->ranges.reserve(n);
+  by_dst.reserve(n);
+  for (int i = 0; i < n; ++i) {
+    if (r[i].n < 0) return fail(ctx, ALORA_EINVAL, "range %d: n = %lld is negative", i, (long long)r[i].n);
+    if (r[i].src < 0 || r[i].n > src_tokens || r[i].src > src_tokens - r[i].n)
+      return fail(ctx, ALORA_ECAPACITY, "range %d: %lld source rows from %lld on lie outside the pool of %lld tokens", i, (long long)r[i].n,
+                  (long long)r[i].src, (long long)src_tokens);
+    if (r[i].dst < 0 || r[i].n > dst_tokens || r[i].dst > dst_tokens - r[i].n)
+      return fail(ctx, ALORA_ECAPACITY, "range %d: %lld destination rows from %lld on lie outside the pool of %lld tokens", i, (long long)r[i].n,
+                  (long long)r[i].dst, (long long)dst_tokens);
+    if (r[i].n == 0) continue;
+    const RowRange q{r[i].src, r[i].dst, r[i].n, 0};
+    by_dst.push_back(q);
+    if (in_place && q.src == q.dst) continue;
+    job->ranges.push_back(q);
+    job->rows += q.n;
+  }
+  std::sort(by_dst.begin(), by_dst.end(), [](const RowRange &x, const RowRange &y) { return x.dst < y.dst; });
+  for (size_t i = 1; i < by_dst.size(); ++i)
+    if (by_dst[i].dst < by_dst[i - 1].dst + by_dst[i - 1].n)
+      return fail(ctx, ALORA_EINVAL, "destination rows [%lld, %lld) and [%lld, %lld) overlap", (long long)by_dst[i - 1].dst,
+                  (long long)(by_dst[i - 1].dst + by_dst[i - 1].n), (long long)by_dst[i].dst, (long long)(by_dst[i].dst + by_dst[i].n));
+  if (in_place && !job->ranges.empty()) {
+    std::vector<RowRange> to(job->ranges), from(job->ranges);
+    std::sort(to.begin(), to.end(), [](const RowRange &x, const RowRange &y) { return x.dst < y.dst; });
+    std::sort(from.begin(), from.end(), [](const RowRange &x, const RowRange &y) { return x.src < y.src; });
+    size_t j = 0;      // destinations are disjoint: in order of their ends as well
+    for (const RowRange &f : from) {
+      while (j < to.size() && to[j].dst + to[j].n <= f.src) ++j;
+      if (j < to.size() && to[j].dst < f.src + f.n) { job->over = true; break; }
+    }
+  }
+  return ALORA_OK;
+}
+
+// Cuts the ranges in pieces of chunk_rows rows; false: too many for a grid.
+bool cut_ranges(std::vector<RowRange> &ranges, int chunk_rows, int64_t *n_chunks) {
+  int64_t n = 0;
+  for (RowRange &q : ranges) { q.first_chunk = n; n += (q.n + chunk_rows - 1) / chunk_rows; }
+  *n_chunks = n;
+  return n <= 0x7fffffff;
+}
+// Rows of a piece: about 32 KB of the widest array
+int chunk_rows_of(int64_t row_bytes) { return (int)std::max<int64_t>(1, std::min<int64_t>(4096, 32768 / std::max<int64_t>(row_bytes, 1))); }
+
+// One launch over ranges x planes: `launch` gets the arguments.
+template <typename F>
+alora_status move_rows(alora_ctx *ctx, std::vector<RowRange> ranges, const std::vector<RowPlane> &planes, int chunk_rows, hipStream_t s, F launch) {
+  if (ranges.empty()) return ALORA_OK;
+  RowsArgs a{};
+  RowsFew few{};
+  a.n_ranges = (int)ranges.size();
+  a.n_planes = (int)planes.size();
+  a.chunk_rows = chunk_rows;
+  if (!cut_ranges(ranges, chunk_rows, &a.n_chunks) || a.n_planes > 65535) return fail(ctx, ALORA_EINVAL, "the call moves more rows than a grid takes");
+  const bool cap = is_capturing(s);
+  MetaSlot *slot = nullptr;
+  if (a.n_ranges <= ROW_FEW_RANGES && a.n_planes <= ROW_FEW_PLANES) {
+    memcpy(few.ranges, ranges.data(), ranges.size() * sizeof(RowRange));
+    memcpy(few.planes, planes.data(), planes.size() * sizeof(RowPlane));
+  } else {
+    if (cap) return fail(ctx, ALORA_EINVAL, "more than %d ranges or %d arrays: not under graph capture", ROW_FEW_RANGES, ROW_FEW_PLANES);
+    const size_t rb = (ranges.size() * sizeof(RowRange) + 15) & ~(size_t)15, pb = (planes.size() * sizeof(RowPlane) + 15) & ~(size_t)15;
+    alora_status st = acquire_slot(ctx, rb + pb, &slot);
+    if (st != ALORA_OK) return st;
+    memcpy(slot->host, ranges.data(), ranges.size() * sizeof(RowRange));
+    memcpy(slot->host + rb, planes.data(), planes.size() * sizeof(RowPlane));
+    const int n16 = (int)((rb + pb) / 16);
+    hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
+    a.ranges = (const RowRange *)slot->dev;
+    a.planes = (const RowPlane *)(slot->dev + rb);
+  }
+  if (cap) {
+    launch(a, few);
+  } else {
+    ProfScope p(ctx, K_ROWS, s);
+    launch(a, few);
+  }
+  HIP_TRY(ctx, hipGetLastError());
+  if (slot) {
+    HIP_TRY(ctx, hipEventRecord(slot->ev, s));
+    slot->in_flight = true;
+  }
+  return ALORA_OK;
+}
+
+int copy_unit(const void *dst, const void *src, int64_t row_bytes) {
+  const uintptr_t m = (uintptr_t)dst | (uintptr_t)src | (uintptr_t)row_bytes;
+  return m % 16 == 0 ? 16 : m % 4 == 0 ? 4 : 1;
+}
+
+// An array of one layer as alora_cache_copy and alora_qcache_copy see it.
+struct CopyArray { const void *src; void *dst; int64_t row_bytes; };
+
+alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int64_t src_tokens, int64_t dst_tokens, const alora_row_range *ranges,
+                       int n_ranges, hipStream_t s) {
+  const bool in_place = arrays[0].dst == arrays[0].src;
+  int64_t widest = 0;
+  for (const CopyArray &c : arrays) {
+    if (!c.dst || !c.src) return fail(ctx, ALORA_EINVAL, "an array of a cache is NULL");
+    if ((c.dst == c.src) != in_place) return fail(ctx, ALORA_EINVAL, "some arrays of dst and src are the same and some are not");
+    const char *d = (const char *)c.dst, *r = (const char *)c.src;
+    if (!in_place && d < r + src_tokens * c.row_bytes && r < d + dst_tokens * c.row_bytes)
+      return fail(ctx, ALORA_EINVAL, "dst and src overlap in memory and are not the same array");
+    widest = std::max(widest, c.row_bytes);
+  }
+  if (in_place && src_tokens != dst_tokens) return fail(ctx, ALORA_EINVAL, "dst and src are the same arrays with different pool_tokens");
+  RowJob job;
+  alora_status st = check_ranges(ctx, ranges, n_ranges, src_tokens, dst_tokens, in_place, &job);
+  if (st != ALORA_OK) return st;
+  if (job.ranges.empty()) return ALORA_OK;
+  if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
+  HIP_TRY(ctx, hipSetDevice(ctx->device));
+  const int chunk = chunk_rows_of(widest);
+  auto copy = [&](const std::vector<RowRange> &r, const std::vector<RowPlane> &planes) {
+    return move_rows(ctx, r, planes, chunk, s, [&](const RowsArgs &a, const RowsFew &few) { launch_rows_copy(a, few, s); });
+  };
+  std::vector<RowPlane> planes;
+  if (!job.over) {
+    for (const CopyArray &c : arrays) planes.push_back(RowPlane{c.src, c.dst, nullptr, c.row_bytes, copy_unit(c.dst, c.src, c.row_bytes)});
+    return copy(job.ranges, planes);
+  }
+  // Rows that move over each other: through the workspace, as many arrays at a time as keep it at 128 MB (half of what the last-level cache holds),
+  // one at least.
+  if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "rows that move over each other: not under graph capture");
+  std::vector<RowRange> out(job.ranges), back(job.ranges);
+  int64_t at = 0;
+  for (size_t i = 0; i < out.size(); ++i) { out[i].dst = at; back[i].src = at; at += out[i].n; }
+  for (size_t i = 0; i < arrays.size();) {
+    size_t j = i, bytes = 0;
+    for (; j < arrays.size(); ++j) {
+      const size_t b = ((size_t)job.rows * arrays[j].row_bytes + 255) & ~(size_t)255;
+      if (j > i && bytes + b > ((size_t)128 << 20)) break;
+      bytes += b;
+    }
+    st = ensure_workspace(ctx, bytes);
+    if (st != ALORA_OK) return st;
+    std::vector<RowPlane> to, from;
+    Bump w(ctx->ws);
+    for (; i < j; ++i) {
+      const CopyArray &c = arrays[i];
+      char *tmp = w.take<char>((size_t)job.rows * c.row_bytes);
+      const int unit = copy_unit(c.dst, c.src, c.row_bytes);
+      to.push_back(RowPlane{c.src, tmp, nullptr, c.row_bytes, unit});
+      from.push_back(RowPlane{tmp, c.dst, nullptr, c.row_bytes, unit});
+    }
+    st = copy(out, to);
+    if (st == ALORA_OK) st = copy(back, from);
+    if (st != ALORA_OK) return st;
+  }
+  return ALORA_OK;
+}
+
+// The arrays of a cache of 4 bits are there, and of the same size in all layers.
+alora_status check_qcaches(alora_ctx *ctx, const alora_qcache *c, int n_layers) {
+  for (int l = 0; l < n_layers; ++l) {
+    if (!c[l].k || !c[l].v || !c[l].k_scale || !c[l].v_scale) return fail(ctx, ALORA_EINVAL, "layer %d: k, v, k_scale or v_scale is NULL", l);
+    if (c[l].pool_tokens != c[0].pool_tokens) return fail(ctx, ALORA_ECAPACITY, "layer %d: pool size differs from layer 0", l);
+  }
+  return ALORA_OK;
+}
+alora_status check_caches(alora_ctx *ctx, const alora_kv_cache *c, int n_layers) {
+  for (int l = 0; l < n_layers; ++l) {
+    if (!c[l].k || !c[l].v) return fail(ctx, ALORA_EINVAL, "layer %d: k or v is NULL", l);
+    if (c[l].pool_tokens != c[0].pool_tokens) return fail(ctx, ALORA_ECAPACITY, "layer %d: pool size differs from layer 0", l);
+  }
+  return ALORA_OK;
+}
+
+// Storing (store) and loading: rows of the storage type in `full`, rows of 4 bits in `four`.
+alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_dim, const alora_qcache *four, const alora_kv_cache *full, bool store,
+                          int n_layers, const alora_row_range *ranges, int n_ranges, hipStream_t s) {
+  if (dtype != ALORA_F32 && dtype != ALORA_BF16) return fail(ctx, ALORA_EDTYPE, "dtype %d is neither ALORA_F32 nor ALORA_BF16", dtype);
+  alora_status st = check_row_shape(ctx, n_kv_heads, head_dim, n_layers, four, full);
+  if (st == ALORA_OK) st = check_qcaches(ctx, four, n_layers);
+  if (st == ALORA_OK) st = check_caches(ctx, full, n_layers);
+  RowJob job;
+  if (st == ALORA_OK)
+    st = store ? check_ranges(ctx, ranges, n_ranges, full->pool_tokens, four->pool_tokens, false, &job)
+               : check_ranges(ctx, ranges, n_ranges, four->pool_tokens, full->pool_tokens, false, &job);
+  if (st != ALORA_OK) return st;
+  const size_t esz = dtype == ALORA_BF16 ? 2 : 4;
+  for (int l = 0; l < n_layers; ++l)
+    for (const void *p : {full[l].k, full[l].v})
+      if ((uintptr_t)p % esz) return fail(ctx, ALORA_EINVAL, "layer %d: k or v is not aligned to its elements", l);
+  if (job.ranges.empty()) return ALORA_OK;
+  if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
+  HIP_TRY(ctx, hipSetDevice(ctx->device));
+  std::vector<RowPlane> planes;
+  planes.reserve((size_t)2 * n_layers);
+  bool wide = head_dim % QBLOCK == 0;
+  for (int l = 0; l < n_layers; ++l)
+    for (int v = 0; v < 2; ++v) {
+      void *f = v ? full[l].v : full[l].k, *q = v ? four[l].v : four[l].k, *e = v ? four[l].v_scale : four[l].k_scale;
+      wide = wide && (((uintptr_t)f | (uintptr_t)q) % 16 == 0);
+      planes.push_back(store ? RowPlane{f, q, e, 0, 0} : RowPlane{q, f, e, 0, 0});
+    }
+  const int chunk = chunk_rows_of((int64_t)n_kv_heads * head_dim * (int64_t)esz);
+  return move_rows(ctx, job.ranges, planes, chunk, s, [&](const RowsArgs &a, const RowsFew &few) {
+    if (store && esz == 2) launch_rows_store<bf16>(a, few, n_kv_heads, head_dim, wide, s);
+    else if (store) launch_rows_store<float>(a, few, n_kv_heads, head_dim, wide, s);
+    else if (esz == 2) launch_rows_load<bf16>(a, few, n_kv_heads, head_dim, wide, s);
+    else launch_rows_load<float>(a, few, n_kv_heads, head_dim, wide, s);
+  });
+}
+
+// Attention over rows of 4 bits: what a call stages for it (after its sequences' records), and its launches.
+struct QAttnPlan {
+  int n_parts = 1;
+  std::vector<int32_t> row_seq;
+  size_t bytes() const { return (row_seq.size() * sizeof(int32_t) + 15) & ~(size_t)15; }
+  void write(char *to) const { memcpy(to, row_seq.data(), row_seq.size() * sizeof(int32_t)); }
+};
+QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L) {
+  QAttnPlan q;
+  q.row_seq.resize(pl.T);
+  for (int b = 0; b < pl.B; ++b)
+    std::fill_n(q.row_seq.begin() + pl.seqs[b].row_start, pl.seqs[b].n_new, b);
+  q.n_parts = pick_splits(ctx, pl.T, L.n_kv_heads, pl.max_len);
+  return q;
+}
+template <typename T>
+void run_qattn(alora_ctx *ctx, const QAttnPlan &q, const char *staged, const LayerDims &L, int T_rows, const QRows &rows, const SeqMeta *seqs_dev,
+               const void *Q, QueryType qt, float *partials, bool decode, T *out, hipStream_t s) {
+  const bool direct = q.n_parts == 1;
+  {
+    ProfScope p(ctx, decode ? K_ATTN_DECODE : K_ATTN_PREFILL, s);
+    launch_qattn_plain<T>(Q, qt, rows, seqs_dev, (const int32_t *)staged, L, T_rows, q.n_parts, partials, direct ? out : nullptr, s);
+  }
+  if (!direct) {
+    ProfScope p(ctx, K_ATTN_MERGE, s);
+    launch_attn_merge<T>(partials, L, T_rows, q.n_parts, MergeCounts{nullptr, 0}, out, s);
+  }
+}
+
+QRows rows_of(const alora_qcache &c) {
+  return QRows{(const uint8_t *)c.k, (const uint8_t *)c.v, (const uint8_t *)c.k_scale, (const uint8_t *)c.v_scale};
+}
+// the sequence tables of a cache of 4 bits as the checks of the other calls take them
+alora_kv_cache table_of(const alora_qcache &c) {
+  return alora_kv_cache{c.k, c.v, c.pool_tokens, c.seq_offset, c.seq_capacity, c.seq_len, c.prefix_offset, c.prefix_len};
+}
+
+alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, int head_dim, const alora_qcache *cache, const void *q,
+                      const int32_t *cu, int B, void *out, hipStream_t s) {
+  if (dtype != ALORA_F32 && dtype != ALORA_BF16) return fail(ctx, ALORA_EDTYPE, "dtype %d is neither ALORA_F32 nor ALORA_BF16", dtype);
+  alora_status st = check_row_shape(ctx, n_kv_heads, head_dim, 1, cache, cache);
+  if (st != ALORA_OK) return st;
+  if (n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % n_kv_heads != 0)
+    return fail(ctx, ALORA_ESHAPE, "n_q_heads = %d must be a positive multiple of n_kv_heads = %d", n_q_heads, n_kv_heads);
+  st = check_qcaches(ctx, cache, 1);
+  if (st != ALORA_OK) return st;
+  if (B < 1) return fail(ctx, ALORA_EINVAL, "B = %d must be at least 1", B);
+  if (!cu) return fail(ctx, ALORA_EINVAL, "cu_seqlens is NULL");
+  if (!cache->seq_offset || !cache->seq_capacity || !cache->seq_len) return fail(ctx, ALORA_EINVAL, "cache seq_offset / seq_capacity / seq_len is NULL");
+  // the checks of the other calls, on the lengths before the rows of the queries
+  std::vector<int32_t> before(B), zero(B, 0), none(B, -1);
+  for (int b = 0; b < B; ++b) {
+    const int S = cu[b + 1] - cu[b], plen = cache->prefix_len ? cache->prefix_len[b] : 0;
+    if (S < 0) return fail(ctx, ALORA_EINVAL, "cu_seqlens decreases at sequence %d", b);
+    if (cache->seq_len[b] < 0) return fail(ctx, ALORA_EINVAL, "seq_len[%d] = %d is negative", b, cache->seq_len[b]);
+    if ((int64_t)S > (int64_t)cache->seq_len[b] - plen && S > 0)
+      return fail(ctx, ALORA_EINVAL, "sequence %d: %d queries, but only %lld rows of its own behind its prefix", b, S, (long long)cache->seq_len[b] - plen);
+    before[b] = cache->seq_len[b] - S;
+  }
+  alora_kv_cache table = table_of(*cache);
+  table.seq_len = before.data();
+  alora_layer_desc ly{};
+  Plan pl;
+  st = check_batch(ctx, &ly, &table, cu, zero.data(), none.data(), B, 1, &pl, false);
+  if (st != ALORA_OK) return st;
+  if (pl.T == 0) return ALORA_OK;
+  if (!q || !out) return fail(ctx, ALORA_EINVAL, "q / out is NULL");
+  const size_t esz = dtype == ALORA_BF16 ? 2 : 4;
+  if ((uintptr_t)q % esz || (uintptr_t)out % esz) return fail(ctx, ALORA_EINVAL, "q / out is not aligned to its elements");
+  if ((int64_t)pl.T * n_q_heads > (1 << 30)) return fail(ctx, ALORA_EINVAL, "%d rows of %d heads are more than one call takes", pl.T, n_q_heads);
+  if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
+  if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "alora_qcache_attend stages its work list from the host: not under graph capture");
+  HIP_TRY(ctx, hipSetDevice(ctx->device));
+  LayerDims L{};
+  L.n_q_heads = n_q_heads; L.n_kv_heads = n_kv_heads; L.head_dim = head_dim;
+  L.n_q = n_q_heads * head_dim; L.n_kv = n_kv_heads * head_dim; L.n_qkv = L.n_q + 2 * L.n_kv;
+  const QAttnPlan qp = plan_qattn(ctx, pl, L);
+  st = ensure_workspace(ctx, qp.n_parts > 1 ? attn_plain_partial_floats(L, pl.T, qp.n_parts) * sizeof(float) : 0);
+  if (st != ALORA_OK) return st;
+  const size_t seq_bytes = ((size_t)B * sizeof(SeqMeta) + 15) & ~(size_t)15;
+  const size_t bytes = seq_bytes + qp.bytes();
+  MetaSlot *slot = nullptr;
+  st = acquire_slot(ctx, bytes, &slot);
+  if (st != ALORA_OK) return st;
+  memcpy(slot->host, pl.seqs.data(), (size_t)B * sizeof(SeqMeta));
+  qp.write(slot->host + seq_bytes);
+  const int n16 = (int)(bytes / 16);
+  hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
+  const SeqMeta *seqs_dev = (const SeqMeta *)slot->dev;
+  if (dtype == ALORA_BF16)
+    run_qattn<bf16>(ctx, qp, slot->dev + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, Q_BF16, (float *)ctx->ws, false, (bf16 *)out, s);
+  else
+    run_qattn<float>(ctx, qp, slot->dev + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, Q_F32, (float *)ctx->ws, false, (float *)out, s);
+  HIP_TRY(ctx, hipGetLastError());
+  HIP_TRY(ctx, hipEventRecord(slot->ev, s));
+  slot->in_flight = true;
+  return ALORA_OK;
+}
+
 alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, alora_kv_cache *caches,
                  const void *x, const int32_t *cu, const int32_t *kps, const int32_t *aps, int B, void *out,
-                 void *stream, bool stack, bool decode = false, int n_steps = 1, bool use_static = false) {
+                 void *stream, bool stack, bool decode = false, int n_steps = 1, bool use_static = false, const alora_qcache *qc = nullptr) {
+  // (qc: caches of 4 bits, whose tables `caches` holds)
   if (!ctx) return ALORA_EINVAL;
   ctx->err.clear();
   if (n_layers < 1) return fail(ctx, ALORA_EINVAL, "n_layers = %d must be at least 1", n_layers);
@@ -1424,7 +1769,13 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
       }
     count_adapted_tiles(&run_pl, 0);
   }
-  const Plan &ppl = run_steps > 1 ? run_pl : pl;      // the rows that are projected together
+  // Caches of 4 bits: the projection appends to a pool of the call's rows alone, in their order, from which they are stored.
+  if (qc) {
+    if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "calls on caches of 4 bits stage their work lists from the host: not under graph capture");
+    run_pl = pl;
+    for (SeqMeta &m : run_pl.seqs) { m.pool_off = (int64_t)m.row_start - m.P; m.prefix_off = 0; m.prefix_len = 0; }
+  }
+  const Plan &ppl = run_steps > 1 || qc ? run_pl : pl;      // the rows that are projected together
   // kernel family: MFMA for bf16 shapes it covers, plain otherwise
   const bool mfma = layers[0].dtype == ALORA_BF16 && ctx->opt_kernels == 0 && L.d % 64 == 0 &&
                     (L.n_adapters == 0 || (L.rank % 8 == 0 && L.n_adapters <= 64)) && L.n_q % 32 == 0 &&
@@ -1456,8 +1807,8 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   // work lists of the MFMA attention kernels (the number of partial records per (row, head) comes out of them)
   const int attn_waves = ctx->opt_attn_waves == 4 ? 4 : 8;
   int n_splits = pick_splits(ctx, pl.T, L.n_kv_heads, pl.max_len);
-  bool attn_mfma = layers[0].dtype == ALORA_BF16 && ctx->opt_kernels == 0 && !decode && attn_prefill_mfma_supported(L);
-  bool decode_mfma = layers[0].dtype == ALORA_BF16 && ctx->opt_kernels == 0 && decode && attn_decode_mfma_supported(L);
+  bool attn_mfma = !qc && layers[0].dtype == ALORA_BF16 && ctx->opt_kernels == 0 && !decode && attn_prefill_mfma_supported(L);
+  bool decode_mfma = !qc && layers[0].dtype == ALORA_BF16 && ctx->opt_kernels == 0 && decode && attn_decode_mfma_supported(L);
   DecodePlan dp;
   PrefillPlan pp;
   auto plan_decode = [&](bool items) {
@@ -1507,6 +1858,8 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     pp = plan_prefill_ranges(ctx, pl, L, B, attn_waves);
     n_splits = pp.n_own + pp.n_sh;
   }
+  QAttnPlan qp;
+  if (qc) { qp = plan_qattn(ctx, pl, L); n_splits = qp.n_parts; }
   const Plan &att_pl = run_prefill ? run_att : pl;      // the rows that attend together: sequence after sequence (the kernel finds where they lie)
   const std::vector<DecItem> &ditems = dp.items;
   const int n_static_items = dp.n_device_items;
@@ -1570,7 +1923,9 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     for (int b = 0; b < B; ++b) caches[0].seq_len[b] += 1;
     return ALORA_OK;
   }
-  st = ensure_workspace(ctx, probe.bytes);
+  // (caches of 4 bits: the new keys and values in the storage type, before they are stored)
+  const size_t new_bytes = qc ? ((size_t)pl.T * L.n_kv * esz + 255) & ~(size_t)255 : 0;
+  st = ensure_workspace(ctx, probe.bytes + 2 * new_bytes);
   if (st != ALORA_OK) return st;
   st = ensure_rope(ctx, pl.max_len, L.head_dim / 2, layers[0].rope_theta, s);
   if (st != ALORA_OK) return st;
@@ -1582,7 +1937,26 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   const size_t row_bytes = ((dp.rows.size() + dp.counts.size() + run_order.size()) * sizeof(int32_t) + 15) & ~(size_t)15;      // decode: shared items' rows, records per row; runs
   const size_t work_bytes = list_bytes + row_bytes;
   const size_t scale_bytes = stack ? (((size_t)L.n_adapters * sizeof(float) + 15) & ~(size_t)15) : 0;
-  const size_t meta_bytes = seq_bytes + work_bytes + scale_bytes;
+  // caches of 4 bits: the sequences' own records, the attention's work list, what is stored where
+  std::vector<RowRange> new_rows;
+  std::vector<RowPlane> new_planes;
+  RowsArgs store{};
+  if (qc) {
+    for (const SeqMeta &m : pl.seqs)
+      if (m.n_new > 0) new_rows.push_back(RowRange{m.row_start, m.pool_off + m.P, m.n_new, 0});
+    store.chunk_rows = chunk_rows_of((int64_t)L.n_kv * (int64_t)esz);
+    if (!cut_ranges(new_rows, store.chunk_rows, &store.n_chunks)) return fail(ctx, ALORA_EINVAL, "the call stores more rows than a grid takes");
+    store.n_ranges = (int)new_rows.size();
+    store.n_planes = 2;
+    for (int l = 0; l < n_layers; ++l) {
+      new_planes.push_back(RowPlane{ctx->ws + probe.bytes, qc[l].k, qc[l].k_scale, 0, 0});
+      new_planes.push_back(RowPlane{ctx->ws + probe.bytes + new_bytes, qc[l].v, qc[l].v_scale, 0, 0});
+    }
+  }
+  const size_t qseq_bytes = qc ? (pl.seqs.size() * sizeof(SeqMeta) + 15) & ~(size_t)15 : 0, qattn_bytes = qc ? qp.bytes() : 0;
+  const size_t range_bytes = (new_rows.size() * sizeof(RowRange) + 15) & ~(size_t)15, plane_bytes = (new_planes.size() * sizeof(RowPlane) + 15) & ~(size_t)15;
+  const size_t q_at = seq_bytes + work_bytes + scale_bytes;
+  const size_t meta_bytes = q_at + qseq_bytes + qattn_bytes + range_bytes + plane_bytes;
   MetaSlot *slot = nullptr;
   st = acquire_slot(ctx, meta_bytes, &slot);
   if (st != ALORA_OK) return st;
@@ -1595,6 +1969,14 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   const size_t order_at = seq_bytes + list_bytes + (dp.counts.size() + dp.rows.size()) * sizeof(int32_t);
   if (!run_order.empty()) memcpy(slot->host + order_at, run_order.data(), run_order.size() * sizeof(int32_t));
   if (scale_bytes) memcpy(slot->host + seq_bytes + work_bytes, layers[0].scale, (size_t)L.n_adapters * sizeof(float));
+  if (qc) {
+    char *at = slot->host + q_at;
+    memcpy(at, pl.seqs.data(), pl.seqs.size() * sizeof(SeqMeta));
+    qp.write(at += qseq_bytes);
+    memcpy(at += qattn_bytes, new_rows.data(), new_rows.size() * sizeof(RowRange));
+    memcpy(at += range_bytes, new_planes.data(), new_planes.size() * sizeof(RowPlane));
+    store.ranges = (const RowRange *)(slot->dev + q_at + qseq_bytes + qattn_bytes);
+  }
   const int n16 = (int)((meta_bytes + 15) / 16);
   const bool carried = ppl.B <= FEW_SEQS && n16 <= STAGE_N16 && !ctx->opt_stage_copy;      // by the call's first kernel
   if (carried) {
@@ -1635,7 +2017,26 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   }
 
   const bool bf = layers[0].dtype == ALORA_BF16;
-  if (!stack) {
+  // the attention block of a layer on caches of 4 bits
+  auto q_block = [&](int l, const auto *cur, auto *attn) {
+    using T = std::remove_pointer_t<decltype(attn)>;
+    alora_kv_cache fresh{};
+    fresh.k = ctx->ws + probe.bytes; fresh.v = ctx->ws + probe.bytes + new_bytes; fresh.pool_tokens = pl.T;
+    project_rows<T>(ctx, &layers[l], L, &fresh, cur, ppl, seqs_dev, w, l == 0, 0, s);
+    const bool wide = L.head_dim % QBLOCK == 0 && ((uintptr_t)qc[l].k | (uintptr_t)qc[l].v) % 16 == 0;
+    store.planes = (const RowPlane *)(slot->dev + q_at + qseq_bytes + qattn_bytes + range_bytes) + 2 * l;
+    {
+      ProfScope p(ctx, K_ROWS, s);
+      launch_rows_store<T>(store, RowsFew{}, L.n_kv_heads, L.head_dim, wide, s);
+    }
+    const QueryForm qf = query_form<T>(ctx, L, w);
+    run_qattn<T>(ctx, qp, slot->dev + q_at + qseq_bytes, L, pl.T, rows_of(qc[l]), (const SeqMeta *)(slot->dev + q_at), w.Q, qf.half ? Q_F16 : Q_F32, w.partials,
+                 decode, attn, s);
+  };
+  if (qc && !stack) {
+    if (bf) q_block(0, (const bf16 *)x, (bf16 *)out);
+    else q_block(0, (const float *)x, (float *)out);
+  } else if (!stack) {
     // n_steps > 1: a run of decode steps on the metadata staged once, projected together (run_steps = n_steps) or one at a time
     auto steps = [&](auto one) {
       using T = decltype(one);
@@ -1653,10 +2054,12 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     for (int l = 0; l < n_layers; ++l) {
       void *nxt = (l == n_layers - 1) ? out : ((l & 1) ? w.xb : w.xa);
       if (bf) {
-        attention_block<bf16>(ctx, &layers[l], L, &caches[l], (const bf16 *)cur, pl, seqs_dev, w, l == 0, n_splits, decode, 0, (bf16 *)w.attn, s);
+        if (qc) q_block(l, (const bf16 *)cur, (bf16 *)w.attn);
+        else attention_block<bf16>(ctx, &layers[l], L, &caches[l], (const bf16 *)cur, pl, seqs_dev, w, l == 0, n_splits, decode, 0, (bf16 *)w.attn, s);
         layer_tail<bf16>(ctx, &layers[l], L, (const bf16 *)cur, w, pl.T, (bf16 *)nxt, s);
       } else {
-        attention_block<float>(ctx, &layers[l], L, &caches[l], (const float *)cur, pl, seqs_dev, w, l == 0, n_splits, decode, 0, (float *)w.attn, s);
+        if (qc) q_block(l, (const float *)cur, (float *)w.attn);
+        else attention_block<float>(ctx, &layers[l], L, &caches[l], (const float *)cur, pl, seqs_dev, w, l == 0, n_splits, decode, 0, (float *)w.attn, s);
         layer_tail<float>(ctx, &layers[l], L, (const float *)cur, w, pl.T, (float *)nxt, s);
       }
       cur = nxt;
@@ -1973,6 +2376,98 @@ alora_status alora_stack_decode(alora_ctx *ctx, const alora_layer_desc *layers, 
   std::vector<int32_t> cu(B + 1);
   for (int b = 0; b <= B; ++b) cu[b] = b;
   return run(ctx, layers, n_layers, caches, x_tok, cu.data(), k_per_seq, adapter_per_seq, B, out, stream, true, true);
+}
+
+alora_status alora_cache_copy(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_kv_cache *dst,
+                              const alora_kv_cache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream) {
+  return guarded(ctx, [&] {
+    if (dtype != ALORA_F32 && dtype != ALORA_BF16) return fail(ctx, ALORA_EDTYPE, "dtype %d is neither ALORA_F32 nor ALORA_BF16", dtype);
+    alora_status st = check_row_shape(ctx, n_kv_heads, head_dim, n_layers, dst, src);
+    if (st == ALORA_OK) st = check_caches(ctx, dst, n_layers);
+    if (st == ALORA_OK) st = check_caches(ctx, src, n_layers);
+    if (st != ALORA_OK) return st;
+    const int64_t row = (int64_t)n_kv_heads * head_dim * (dtype == ALORA_BF16 ? 2 : 4);
+    std::vector<CopyArray> arrays;
+    for (int l = 0; l < n_layers; ++l) {
+      arrays.push_back(CopyArray{src[l].k, dst[l].k, row});
+      arrays.push_back(CopyArray{src[l].v, dst[l].v, row});
+    }
+    return copy_rows(ctx, arrays, src->pool_tokens, dst->pool_tokens, ranges, n_ranges, (hipStream_t)stream);
+  });
+}
+
+alora_status alora_qcache_copy(alora_ctx *ctx, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *dst, const alora_qcache *src,
+                               int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream) {
+  return guarded(ctx, [&] {
+    alora_status st = check_row_shape(ctx, n_kv_heads, head_dim, n_layers, dst, src);
+    if (st == ALORA_OK) st = check_qcaches(ctx, dst, n_layers);
+    if (st == ALORA_OK) st = check_qcaches(ctx, src, n_layers);
+    if (st != ALORA_OK) return st;
+    const int64_t codes = (int64_t)n_kv_heads * (head_dim / 2), scales = (int64_t)n_kv_heads * q_blocks(head_dim);
+    std::vector<CopyArray> arrays;
+    for (int l = 0; l < n_layers; ++l) {
+      arrays.push_back(CopyArray{src[l].k, dst[l].k, codes});
+      arrays.push_back(CopyArray{src[l].v, dst[l].v, codes});
+      arrays.push_back(CopyArray{src[l].k_scale, dst[l].k_scale, scales});
+      arrays.push_back(CopyArray{src[l].v_scale, dst[l].v_scale, scales});
+    }
+    return copy_rows(ctx, arrays, src->pool_tokens, dst->pool_tokens, ranges, n_ranges, (hipStream_t)stream);
+  });
+}
+
+alora_status alora_qcache_store(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *dst,
+                                const alora_kv_cache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream) {
+  return guarded(ctx, [&] { return convert_rows(ctx, dtype, n_kv_heads, head_dim, dst, src, true, n_layers, ranges, n_ranges, (hipStream_t)stream); });
+}
+
+alora_status alora_qcache_load(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_kv_cache *dst,
+                               const alora_qcache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream) {
+  return guarded(ctx, [&] { return convert_rows(ctx, dtype, n_kv_heads, head_dim, src, dst, false, n_layers, ranges, n_ranges, (hipStream_t)stream); });
+}
+
+alora_status alora_qcache_attend(alora_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *cache,
+                                 const void *q, const int32_t *cu_seqlens, int32_t B, void *out, void *stream) {
+  return guarded(ctx, [&] { return attend_q(ctx, dtype, n_q_heads, n_kv_heads, head_dim, cache, q, cu_seqlens, B, out, (hipStream_t)stream); });
+}
+
+// prefill, decode and the stacks on caches of 4 bits: the same host code as on the others
+static alora_status run_q(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, alora_qcache *caches, const void *x, const int32_t *cu,
+                          const int32_t *kps, const int32_t *aps, int B, void *out, void *stream, bool stack, bool decode) {
+  return guarded(ctx, [&] {
+    if (n_layers < 1) return fail(ctx, ALORA_EINVAL, "n_layers = %d must be at least 1", n_layers);
+    if (!layers || !caches) return fail(ctx, ALORA_EINVAL, "layers / caches is NULL");
+    if (decode && B < 1) return fail(ctx, ALORA_EINVAL, "B = %d must be at least 1", B);
+    alora_status st = check_qcaches(ctx, caches, n_layers);
+    if (st != ALORA_OK) return st;
+    std::vector<int32_t> one;
+    if (decode)
+      for (int b = 0; b <= B; ++b) one.push_back(b);
+    std::vector<alora_kv_cache> tables;
+    for (int l = 0; l < n_layers; ++l) tables.push_back(table_of(caches[l]));
+    return run(ctx, layers, n_layers, tables.data(), x, decode ? one.data() : cu, kps, aps, B, out, stream, stack, decode, 1, false, caches);
+  });
+}
+
+alora_status alora_qcache_prefill(alora_ctx *ctx, const alora_layer_desc *layer, alora_qcache *cache, const void *x_suffix,
+                                  const int32_t *cu_seqlens, const int32_t *k_per_seq, const int32_t *adapter_per_seq, int32_t B,
+                                  void *attn_out, void *stream) {
+  return run_q(ctx, layer, 1, cache, x_suffix, cu_seqlens, k_per_seq, adapter_per_seq, B, attn_out, stream, false, false);
+}
+
+alora_status alora_qcache_decode(alora_ctx *ctx, const alora_layer_desc *layer, alora_qcache *cache, const void *x_tok, const int32_t *k_per_seq,
+                                 const int32_t *adapter_per_seq, int32_t B, void *attn_out, void *stream) {
+  return run_q(ctx, layer, 1, cache, x_tok, nullptr, k_per_seq, adapter_per_seq, B, attn_out, stream, false, true);
+}
+
+alora_status alora_qcache_stack_prefill(alora_ctx *ctx, const alora_layer_desc *layers, int32_t n_layers, alora_qcache *caches, const void *x,
+                                        const int32_t *cu_seqlens, const int32_t *k_per_seq, const int32_t *adapter_per_seq, int32_t B,
+                                        void *out, void *stream) {
+  return run_q(ctx, layers, n_layers, caches, x, cu_seqlens, k_per_seq, adapter_per_seq, B, out, stream, true, false);
+}
+
+alora_status alora_qcache_stack_decode(alora_ctx *ctx, const alora_layer_desc *layers, int32_t n_layers, alora_qcache *caches, const void *x_tok,
+                                       const int32_t *k_per_seq, const int32_t *adapter_per_seq, int32_t B, void *out, void *stream) {
+  return run_q(ctx, layers, n_layers, caches, x_tok, nullptr, k_per_seq, adapter_per_seq, B, out, stream, true, true);
 }
 
 }  // extern "C"

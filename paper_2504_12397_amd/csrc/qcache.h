@@ -1,0 +1,50 @@
+// Launchers of the kernels on cached rows: copying them, storing them in 4 bits and loading them again, attention over them.
+#pragma once
+#include "common.h"
+
+namespace alora {
+
+// ---- rows of 4 bits -------------------------------------------------------------------------------------
+// A row holds head_dim codes of 4 bits per kv head (sign and e2m1 magnitude: 0, 0.5, 1, 1.5, 2, 3, 4, 6; element 2i in the low half of
+// byte i) and one exponent byte E for each QBLOCK channels (the last block of a head may be shorter): value = code * 2^(E - 127).
+constexpr int QBLOCK = 32;
+constexpr int Q_E_MIN = 2, Q_E_MAX = 252, Q_E_NAN = 255;      // (every value and half of the smallest one are normal fp32 and bf16 numbers)
+__host__ __device__ inline int q_blocks(int head_dim) { return (head_dim + QBLOCK - 1) / QBLOCK; }
+
+// ---- moving rows (alora_cache_copy, alora_qcache_copy / store / load) ------------------------------------
+// One array per layer and kind of data (keys, values; codes and exponents): row r begins at base + r * row_bytes.  Storing and
+// loading use dst and src for the rows of 4 bits and of the storage type, `scale` for the exponents.
+struct RowPlane {
+  const void *src;
+  void *dst;
+  void *scale;             // store: written; load: read
+  int64_t row_bytes;       // copy ...
+  int64_t unit;            // ... in pieces of 16, 4 or 1 bytes, which both bases and the rows are multiples of
+};
+// n rows from src on go to dst on; first_chunk: how many pieces of chunk_rows rows the ranges before it are cut in
+struct RowRange { int64_t src, dst, n, first_chunk; };
+// Few planes and ranges travel as kernel arguments (no staging kernel before the copy, and a captured call keeps them); more of them in device memory.
+constexpr int ROW_FEW_RANGES = 16, ROW_FEW_PLANES = 64;
+struct RowsFew { RowRange ranges[ROW_FEW_RANGES]; RowPlane planes[ROW_FEW_PLANES]; };
+struct RowsArgs {
+  const RowRange *ranges;        // both nullptr: in `few`
+  const RowPlane *planes;
+  int n_ranges, n_planes;
+  int64_t n_chunks;              // of all ranges
+  int chunk_rows;
+};
+void launch_rows_copy(const RowsArgs &a, const RowsFew &few, hipStream_t s);
+// T rows of n_kv heads of head_dim <-> rows of 4 bits; wide: head_dim is a multiple of 32 and every base of 16 bytes (exponents: of 4)
+template <typename T> void launch_rows_store(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);
+template <typename T> void launch_rows_load(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);
+
+// ---- attention over rows of 4 bits ---------------------------------------------------------------------------
+struct QRows { const uint8_t *k, *v, *k_scale, *v_scale; };      // pool arrays of one layer
+enum QueryType { Q_F32 = 0, Q_BF16 = 1, Q_F16 = 2 };
+
+// any even head size: a wave per (row, query head, part); row_seq[T]: the row's sequence.  out: the result itself, with n_splits == 1 only
+template <typename T>
+void launch_qattn_plain(const void *Q, QueryType qt, const QRows &c, const SeqMeta *seqs, const int32_t *row_seq, const LayerDims &L, int T_rows,
+                        int n_splits, float *partials, T *out, hipStream_t s);
+
+}  // namespace alora
