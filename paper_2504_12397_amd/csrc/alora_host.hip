@@ -1588,32 +1588,163 @@ alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_di
   });
 }
 
-// Attention over rows of 4 bits: what a call stages for it (after its sequences' records), and its launches.
-struct QAttnPlan {
-  int n_parts = 1;
-  std::vector<int32_t> row_seq;
-  size_t bytes() const { return (row_seq.size() * sizeof(int32_t) + 15) & ~(size_t)15; }
-  void write(char *to) const { memcpy(to, row_seq.data(), row_seq.size() * sizeof(int32_t)); }
+// Attention over rows of 4 bits: what a call stages for it (after its sequences' records), and its launches.  On the matrix units, the rows that read
+// the same keys -- a sequence's own, or a shared prefix of several sequences -- are a unit; its (row, query head) pairs are columns.  Units of up to 16
+// columns (single tokens) and the others are launched apart, each class with the shape of workgroup that suits it.
+struct QAttnClass {
+  int nc = 1, hw = 1, kr = 1, cw = 1;
+  std::vector<QAttnItem> items;
 };
-QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L) {
+struct QAttnPlan {
+  bool mfma = false;
+  int n_parts = 1, first_shared = 0;
+  std::vector<int32_t> row_seq;          // plain kernel: every row's sequence
+  QAttnClass cls[2];
+  std::vector<int32_t> rows, counts;     // rows of the shared units; records per row, own and shared
+  static size_t up(size_t b) { return (b + 15) & ~(size_t)15; }
+  size_t item_bytes() const { return up((cls[0].items.size() + cls[1].items.size()) * sizeof(QAttnItem)); }
+  size_t bytes() const { return up(row_seq.size() * 4) + item_bytes() + up(rows.size() * 4) + up(counts.size() * 4); }
+  void write(char *to) const {
+    auto put = [&](const void *p, size_t n, size_t room) { if (n) memcpy(to, p, n); to += room; };
+    put(row_seq.data(), row_seq.size() * 4, up(row_seq.size() * 4));
+    const size_t n0 = cls[0].items.size() * sizeof(QAttnItem), n1 = cls[1].items.size() * sizeof(QAttnItem);
+    put(cls[0].items.data(), n0, n0);
+    put(cls[1].items.data(), n1, item_bytes() - n0);
+    put(rows.data(), rows.size() * 4, up(rows.size() * 4));
+    put(counts.data(), counts.size() * 4, up(counts.size() * 4));
+  }
+};
+int qattn_ht(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+bool qattn_mfma_supported(const alora_ctx *ctx, const LayerDims &L, const alora_qcache &c, const void *q, const void *out) {
+  return ctx->opt_kernels == 0 && L.head_dim % 8 == 0 && (((uintptr_t)c.k | (uintptr_t)c.v) & 3) == 0 && (((uintptr_t)q | (uintptr_t)out) & 15) == 0 &&
+         (int64_t)L.n_kv * 64 < (1 << 30);      // (offsets of a step's rows in 32 bits)
+}
+
+QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, QueryType qt, bool mfma) {
   QAttnPlan q;
-  q.row_seq.resize(pl.T);
-  for (int b = 0; b < pl.B; ++b)
-    std::fill_n(q.row_seq.begin() + pl.seqs[b].row_start, pl.seqs[b].n_new, b);
-  q.n_parts = pick_splits(ctx, pl.T, L.n_kv_heads, pl.max_len);
+  q.mfma = mfma;
+  if (!mfma) {
+    q.row_seq.resize(pl.T);
+    for (int b = 0; b < pl.B; ++b)
+      std::fill_n(q.row_seq.begin() + pl.seqs[b].row_start, pl.seqs[b].n_new, b);
+    q.n_parts = pick_splits(ctx, pl.T, L.n_kv_heads, pl.max_len);
+    return q;
+  }
+  const int G = L.n_q_heads / L.n_kv_heads, ht = qattn_ht(L.head_dim);
+  const int nc_most = qt == Q_F32 ? 1 : ht == 256 ? 1 : qt == Q_F16 ? 2 : ht == 64 ? 4 : 2;
+  struct Unit { int64_t row0; int len, first, n_rows, pos0; bool shared; };
+  std::vector<Unit> units[2];
+  auto add = [&](const Unit &u) { units[(int64_t)u.n_rows * G > 16 ? 1 : 0].push_back(u); };
+  for (const SeqMeta &m : pl.seqs)
+    if (m.n_new > 0) add(Unit{m.pool_off + m.prefix_len, m.P - m.prefix_len + m.n_new, m.row_start, m.n_new, m.P - m.prefix_len, false});
+  if (pl.any_prefix) {
+    const std::vector<int32_t> order = by_prefix(pl);
+    int first = 0;
+    for (int i = 0; i < pl.B; ++i) {
+      const SeqMeta &m = pl.seqs[order[i]];
+      const bool goes_on = i > 0 && pl.seqs[order[i - 1]].prefix_off == m.prefix_off && pl.seqs[order[i - 1]].prefix_len == m.prefix_len;
+      if (!goes_on) first = (int)q.rows.size();
+      if (m.prefix_len > 0)
+        for (int r = 0; r < m.n_new; ++r) q.rows.push_back(m.row_start + r);
+      const bool last = i + 1 == pl.B || pl.seqs[order[i + 1]].prefix_off != m.prefix_off || pl.seqs[order[i + 1]].prefix_len != m.prefix_len;
+      if (last && (int)q.rows.size() > first) add(Unit{m.prefix_off, m.prefix_len, first, (int)q.rows.size() - first, 0, true});
+    }
+  }
+  const int cap = pl.T <= 16 ? 256 : std::max(1, std::min(64, 8192 / pl.T));      // most records of a kind that a row has (memory of the records)
+  int range[2] = {1, 1};
+  for (int k = 0; k < 2; ++k) {
+    if (units[k].empty()) continue;
+    QAttnClass &c = q.cls[k];
+    int64_t cols = 0, longest = 0;
+    for (const Unit &u : units[k]) { cols = std::max(cols, (int64_t)u.n_rows * G); longest = std::max<int64_t>(longest, u.len); }
+    c.nc = (int)std::min<int64_t>(nc_most, cols <= 16 ? 1 : cols <= 32 ? 2 : 4);
+    while (c.cw < 4 && 16 * c.nc * c.cw < cols) c.cw *= 2;
+    c.hw = 8 / c.cw;
+    while (c.hw > 1 && c.hw / 2 >= L.n_kv_heads) c.hw /= 2;
+    const int slots = ctx->n_cu;
+    auto items_of = [&](int hw, int64_t r) {
+      int64_t n = 0;
+      for (const Unit &u : units[k])
+        n += ((u.len + r - 1) / r) * (((int64_t)u.n_rows * G + 16 * c.nc * c.cw - 1) / (16 * c.nc * c.cw)) * ((L.n_kv_heads + hw - 1) / hw);
+      return n;
+    };
+    // while even ranges of 32 keys a wave leave half of the chip idle, more waves share a head's keys
+    while (c.hw > 1 && items_of(c.hw, 32 * (8 / (c.hw * c.cw))) * 2 <= slots) c.hw /= 2;
+    c.kr = 8 / (c.hw * c.cw);
+    int64_t r = std::max<int64_t>((longest + cap - 1) / cap, 128 * c.kr);
+    if (ctx->opt_splits > 0) {
+      r = std::max<int64_t>(1, (longest + ctx->opt_splits - 1) / ctx->opt_splits);
+    } else {
+      for (int i = 0; i < 64 && r < longest && items_of(c.hw, r) > slots; ++i) r += std::max<int64_t>(32, r / 16);
+    }
+    r = std::min((r + 31) & ~(int64_t)31, (longest + 31) & ~(int64_t)31);
+    range[k] = (int)r;
+  }
+  int n_own = 1, n_shared = 0;
+  for (int k = 0; k < 2; ++k)
+    for (const Unit &u : units[k]) (u.shared ? n_shared : n_own) = std::max(u.shared ? n_shared : n_own, (u.len + range[k] - 1) / range[k]);
+  q.n_parts = n_own + n_shared;
+  q.first_shared = n_own;
+  if (q.n_parts > 1) q.counts.assign((size_t)2 * pl.T, 0);
+  for (int k = 0; k < 2; ++k) {
+    QAttnClass &c = q.cls[k];
+    const int wide = 16 * c.nc * c.cw;
+    for (const Unit &u : units[k]) {
+      const int r = range[k], cols = u.n_rows * G;
+      if (q.n_parts > 1)
+        for (int i = 0; i < u.n_rows; ++i) {
+          if (u.shared) q.counts[2 * q.rows[u.first + i] + 1] = (u.len + r - 1) / r;
+          else q.counts[2 * (u.first + i)] = (u.pos0 + i + 1 + r - 1) / r;
+        }
+      for (int col0 = 0; col0 < cols; col0 += wide) {
+        const int n = std::min(wide, cols - col0), end = u.shared ? u.len : std::min(u.len, u.pos0 + (col0 + n - 1) / G + 1);
+        for (int at = 0, p = 0; at < end; at += r, ++p)
+          for (int g = 0; g < L.n_kv_heads; g += c.hw)
+            c.items.push_back(QAttnItem{u.row0, at, std::min(end, at + r), u.first, col0, n, u.pos0, g, (u.shared ? n_own : 0) + p, u.shared ? 1 : 0, 0});
+      }
+    }
+    // longest first, so that the short ones even out the end
+    auto longer = [](const QAttnItem &x, const QAttnItem &y) { return x.kend - x.kbeg > y.kend - y.kbeg; };
+    if (!std::is_sorted(c.items.begin(), c.items.end(), longer)) std::stable_sort(c.items.begin(), c.items.end(), longer);
+  }
   return q;
 }
 template <typename T>
 void run_qattn(alora_ctx *ctx, const QAttnPlan &q, const char *staged, const LayerDims &L, int T_rows, const QRows &rows, const SeqMeta *seqs_dev,
                const void *Q, QueryType qt, float *partials, bool decode, T *out, hipStream_t s) {
   const bool direct = q.n_parts == 1;
+  MergeCounts mc{nullptr, 0};
   {
     ProfScope p(ctx, decode ? K_ATTN_DECODE : K_ATTN_PREFILL, s);
-    launch_qattn_plain<T>(Q, qt, rows, seqs_dev, (const int32_t *)staged, L, T_rows, q.n_parts, partials, direct ? out : nullptr, s);
+    if (!q.mfma) {
+      launch_qattn_plain<T>(Q, qt, rows, seqs_dev, (const int32_t *)staged, L, T_rows, q.n_parts, partials, direct ? out : nullptr, s);
+    } else {
+      QAttnArgs a{};
+      a.Q = Q; a.c = rows;
+      a.items = (const QAttnItem *)staged;
+      a.rows = (const int32_t *)(staged + q.item_bytes());
+      a.n_q_heads = L.n_q_heads; a.n_kv_heads = L.n_kv_heads; a.head_dim = L.head_dim;
+      a.n_parts = q.n_parts;
+      a.sm_scale = 1.0f / sqrtf((float)L.head_dim);
+      a.partials = partials;
+      a.out = direct ? out : nullptr;
+      if (!direct) mc = MergeCounts{(const int32_t *)(staged + q.item_bytes() + QAttnPlan::up(q.rows.size() * 4)), q.first_shared};
+      for (int k = 0; k < 2; ++k) {
+        const QAttnClass &c = q.cls[k];
+        const int n = (int)c.items.size();
+        if (n == 0) continue;
+        a.hw = c.hw; a.kr = c.kr; a.cw = c.cw;
+        const int ht = qattn_ht(L.head_dim);
+        if (qt == Q_BF16) launch_qattn_mfma_bf16(a, n, ht, c.nc, s);
+        else if (qt == Q_F16) launch_qattn_mfma_f16(a, n, ht, c.nc, s);
+        else launch_qattn_mfma_f32(a, n, ht, c.nc, s);
+        a.items += n;
+      }
+    }
   }
   if (!direct) {
     ProfScope p(ctx, K_ATTN_MERGE, s);
-    launch_attn_merge<T>(partials, L, T_rows, q.n_parts, MergeCounts{nullptr, 0}, out, s);
+    launch_attn_merge<T>(partials, L, T_rows, q.n_parts, mc, out, s);
   }
 }
 
@@ -1664,7 +1795,8 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   LayerDims L{};
   L.n_q_heads = n_q_heads; L.n_kv_heads = n_kv_heads; L.head_dim = head_dim;
   L.n_q = n_q_heads * head_dim; L.n_kv = n_kv_heads * head_dim; L.n_qkv = L.n_q + 2 * L.n_kv;
-  const QAttnPlan qp = plan_qattn(ctx, pl, L);
+  const QueryType qt = dtype == ALORA_BF16 ? Q_BF16 : Q_F32;
+  const QAttnPlan qp = plan_qattn(ctx, pl, L, qt, qattn_mfma_supported(ctx, L, *cache, q, out));
   st = ensure_workspace(ctx, qp.n_parts > 1 ? attn_plain_partial_floats(L, pl.T, qp.n_parts) * sizeof(float) : 0);
   if (st != ALORA_OK) return st;
   const size_t seq_bytes = ((size_t)B * sizeof(SeqMeta) + 15) & ~(size_t)15;
@@ -1678,9 +1810,9 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
   const SeqMeta *seqs_dev = (const SeqMeta *)slot->dev;
   if (dtype == ALORA_BF16)
-    run_qattn<bf16>(ctx, qp, slot->dev + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, Q_BF16, (float *)ctx->ws, false, (bf16 *)out, s);
+    run_qattn<bf16>(ctx, qp, slot->dev + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, false, (bf16 *)out, s);
   else
-    run_qattn<float>(ctx, qp, slot->dev + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, Q_F32, (float *)ctx->ws, false, (float *)out, s);
+    run_qattn<float>(ctx, qp, slot->dev + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, false, (float *)out, s);
   HIP_TRY(ctx, hipGetLastError());
   HIP_TRY(ctx, hipEventRecord(slot->ev, s));
   slot->in_flight = true;
@@ -1859,7 +1991,16 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     n_splits = pp.n_own + pp.n_sh;
   }
   QAttnPlan qp;
-  if (qc) { qp = plan_qattn(ctx, pl, L); n_splits = qp.n_parts; }
+  bool q_half = false;      // (caches of 4 bits: queries travel as fp16, as elsewhere, or as fp32)
+  if (qc) {
+    bool q_mfma = true;
+    for (int l = 0; l < n_layers; ++l) q_mfma = q_mfma && qattn_mfma_supported(ctx, L, qc[l], nullptr, stack ? nullptr : out);
+    q_half = q_mfma && layers[0].dtype == ALORA_BF16;
+    // (the plain kernels take bf16 layers' queries as fp32)
+    if (layers[0].dtype == ALORA_BF16 && !q_half) q_mfma = false;
+    qp = plan_qattn(ctx, pl, L, q_half ? Q_F16 : Q_F32, q_mfma);
+    n_splits = qp.n_parts;
+  }
   const Plan &att_pl = run_prefill ? run_att : pl;      // the rows that attend together: sequence after sequence (the kernel finds where they lie)
   const std::vector<DecItem> &ditems = dp.items;
   const int n_static_items = dp.n_device_items;
@@ -1995,7 +2136,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   w.lora_split = (k_splits > 1 && ctx->opt_lora_split != 2) || ctx->opt_lora_split == 1 ? 1 : 0;
   w.attn_mfma = attn_mfma;
   if (run_prefill) { w.run_steps = n_steps; w.run_seqs = B; w.run_order = run_order.empty() ? nullptr : (const int32_t *)(slot->dev + order_at); }
-  w.decode_mfma = decode_mfma;
+  w.decode_mfma = decode_mfma || q_half;      // (the form of the queries)
   w.attn_waves = attn_waves;
   w.qtiles = (const AttnItem *)(slot->dev + seq_bytes);
   w.n_qtiles = (int)qtiles.size();

@@ -47,4 +47,33 @@ template <typename T>
 void launch_qattn_plain(const void *Q, QueryType qt, const QRows &c, const SeqMeta *seqs, const int32_t *row_seq, const LayerDims &L, int T_rows,
                         int n_splits, float *partials, T *out, hipStream_t s);
 
+// Head sizes that are multiples of 8, on the matrix units.  A workgroup of eight waves is hw kv heads x kr shares of the item's keys x cw
+// groups of 16 * nc columns; a column is a (row, query head) pair: column c of a unit is head c % G of its row c / G.
+struct QAttnItem {
+  int64_t key_row0;         // pool row of key 0
+  int32_t kbeg, kend;       // keys, counted from key_row0; none beyond kend is read
+  int32_t first_row;        // own keys: packed row of the unit's row 0; shared: where the unit's rows begin in QAttnArgs::rows
+  int32_t col0, n_cols;     // columns of the unit that this item takes
+  int32_t pos0;             // own keys: the last key that row 0 sees (row i: pos0 + i); shared: every row sees all
+  int32_t g0, part;         // first kv head; which of the n_parts partial records of a (row, head) it writes
+  int32_t shared, pad_;
+};
+static_assert(sizeof(QAttnItem) == 48, "");
+struct QAttnArgs {
+  const void *Q;            // [T, n_q_heads, head_dim]
+  QRows c;
+  const QAttnItem *items;
+  const int32_t *rows;      // packed rows of the shared units
+  int n_q_heads, n_kv_heads, head_dim;
+  int hw, kr, cw;
+  int n_parts;
+  float sm_scale;
+  float *partials;          // [T, n_q_heads, n_parts, head_dim + 2] (sums, maximum, sum of probabilities), used when out == nullptr
+  void *out;                // [T, n_q_heads, head_dim], with n_parts == 1 only
+};
+// ht: 64, 128 or 256, the smallest that holds head_dim.  Codes begin at multiples of 4 bytes, queries and results of 16.
+void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, hipStream_t s);      // queries of bf16; nc 1, 2 or 4 (ht 256: 1, 2)
+void launch_qattn_mfma_f16(const QAttnArgs &a, int n_items, int ht, int nc, hipStream_t s);       // of fp16; nc 1 or 2 (ht 256: 1)
+void launch_qattn_mfma_f32(const QAttnArgs &a, int n_items, int ht, int nc, hipStream_t s);       // of fp32; nc 1
+
 }  // namespace alora
