@@ -1596,7 +1596,7 @@ struct QAttnClass {
   std::vector<QAttnItem> items;
 };
 struct QAttnPlan {
-  bool mfma = false;
+  bool mfma = false, lds = false;
   int n_parts = 1, first_shared = 0;
   std::vector<int32_t> row_seq;          // plain kernel: every row's sequence
   QAttnClass cls[2];
@@ -1620,9 +1620,15 @@ bool qattn_mfma_supported(const alora_ctx *ctx, const LayerDims &L, const alora_
          (int64_t)L.n_kv * 64 < (1 << 30);      // (offsets of a step's rows in 32 bits)
 }
 
-QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, QueryType qt, bool mfma) {
+bool qattn_lds_supported(const LayerDims &L, const alora_qcache &c) {
+  return (L.head_dim == 128 || (L.head_dim == 64 && L.n_kv_heads % 2 == 0)) && (((uintptr_t)c.k | (uintptr_t)c.v) & 15) == 0 &&
+         (((uintptr_t)c.k_scale | (uintptr_t)c.v_scale) & 3) == 0;
+}
+
+QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, QueryType qt, bool mfma, bool lds) {
   QAttnPlan q;
   q.mfma = mfma;
+  q.lds = lds;
   if (!mfma) {
     q.row_seq.resize(pl.T);
     for (int b = 0; b < pl.B; ++b)
@@ -1658,8 +1664,9 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
     int64_t cols = 0, longest = 0;
     for (const Unit &u : units[k]) { cols = std::max(cols, (int64_t)u.n_rows * G); longest = std::max<int64_t>(longest, u.len); }
     c.nc = (int)std::min<int64_t>(nc_most, cols <= 16 ? 1 : cols <= 32 ? 2 : 4);
+    const int waves = qattn_waves(ht);
     while (c.cw < 4 && 16 * c.nc * c.cw < cols) c.cw *= 2;
-    c.hw = 8 / c.cw;
+    c.hw = waves / c.cw;
     while (c.hw > 1 && c.hw / 2 >= L.n_kv_heads) c.hw /= 2;
     const int slots = ctx->n_cu;
     auto items_of = [&](int hw, int64_t r) {
@@ -1669,8 +1676,8 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
       return n;
     };
     // while even ranges of 32 keys a wave leave half of the chip idle, more waves share a head's keys
-    while (c.hw > 1 && items_of(c.hw, 32 * (8 / (c.hw * c.cw))) * 2 <= slots) c.hw /= 2;
-    c.kr = 8 / (c.hw * c.cw);
+    while (c.hw > 1 && items_of(c.hw, 32 * (waves / (c.hw * c.cw))) * 2 <= slots) c.hw /= 2;
+    c.kr = waves / (c.hw * c.cw);
     int64_t r = std::max<int64_t>((longest + cap - 1) / cap, 128 * c.kr);
     if (ctx->opt_splits > 0) {
       r = std::max<int64_t>(1, (longest + ctx->opt_splits - 1) / ctx->opt_splits);
@@ -1735,9 +1742,9 @@ void run_qattn(alora_ctx *ctx, const QAttnPlan &q, const char *staged, const Lay
         if (n == 0) continue;
         a.hw = c.hw; a.kr = c.kr; a.cw = c.cw;
         const int ht = qattn_ht(L.head_dim);
-        if (qt == Q_BF16) launch_qattn_mfma_bf16(a, n, ht, c.nc, s);
-        else if (qt == Q_F16) launch_qattn_mfma_f16(a, n, ht, c.nc, s);
-        else launch_qattn_mfma_f32(a, n, ht, c.nc, s);
+        if (qt == Q_BF16) launch_qattn_mfma_bf16(a, n, ht, c.nc, q.lds, s);
+        else if (qt == Q_F16) launch_qattn_mfma_f16(a, n, ht, c.nc, q.lds, s);
+        else launch_qattn_mfma_f32(a, n, ht, c.nc, q.lds, s);
         a.items += n;
       }
     }
@@ -1796,7 +1803,7 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   L.n_q_heads = n_q_heads; L.n_kv_heads = n_kv_heads; L.head_dim = head_dim;
   L.n_q = n_q_heads * head_dim; L.n_kv = n_kv_heads * head_dim; L.n_qkv = L.n_q + 2 * L.n_kv;
   const QueryType qt = dtype == ALORA_BF16 ? Q_BF16 : Q_F32;
-  const QAttnPlan qp = plan_qattn(ctx, pl, L, qt, qattn_mfma_supported(ctx, L, *cache, q, out));
+  const QAttnPlan qp = plan_qattn(ctx, pl, L, qt, qattn_mfma_supported(ctx, L, *cache, q, out), qattn_lds_supported(L, *cache));
   st = ensure_workspace(ctx, qp.n_parts > 1 ? attn_plain_partial_floats(L, pl.T, qp.n_parts) * sizeof(float) : 0);
   if (st != ALORA_OK) return st;
   const size_t seq_bytes = ((size_t)B * sizeof(SeqMeta) + 15) & ~(size_t)15;
@@ -1993,12 +2000,15 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   QAttnPlan qp;
   bool q_half = false;      // (caches of 4 bits: queries travel as fp16, as elsewhere, or as fp32)
   if (qc) {
-    bool q_mfma = true;
-    for (int l = 0; l < n_layers; ++l) q_mfma = q_mfma && qattn_mfma_supported(ctx, L, qc[l], nullptr, stack ? nullptr : out);
+    bool q_mfma = true, q_lds = true;
+    for (int l = 0; l < n_layers; ++l) {
+      q_mfma = q_mfma && qattn_mfma_supported(ctx, L, qc[l], nullptr, stack ? nullptr : out);
+      q_lds = q_lds && qattn_lds_supported(L, qc[l]);
+    }
     q_half = q_mfma && layers[0].dtype == ALORA_BF16;
     // (the plain kernels take bf16 layers' queries as fp32)
     if (layers[0].dtype == ALORA_BF16 && !q_half) q_mfma = false;
-    qp = plan_qattn(ctx, pl, L, q_half ? Q_F16 : Q_F32, q_mfma);
+    qp = plan_qattn(ctx, pl, L, q_half ? Q_F16 : Q_F32, q_mfma, q_lds);
     n_splits = qp.n_parts;
   }
   const Plan &att_pl = run_prefill ? run_att : pl;      // the rows that attend together: sequence after sequence (the kernel finds where they lie)

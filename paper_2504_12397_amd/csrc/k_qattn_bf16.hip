@@ -3,13 +3,18 @@
 
 namespace alora {
 
-void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, hipStream_t s) {
-  if (ht == 64 && nc == 4) return qattn_mfma_start<64, 1, 2, 4, 1, bf16, bf16>(a, n_items, s);
-  if (ht == 64 && nc == 2) return qattn_mfma_start<64, 1, 2, 2, 3, bf16, bf16>(a, n_items, s);
-  if (ht == 64 && nc == 1) return qattn_mfma_start<64, 1, 2, 1, 4, bf16, bf16>(a, n_items, s);
-  if (ht == 128 && nc == 2) return qattn_mfma_start<128, 1, 2, 2, 2, bf16, bf16>(a, n_items, s);
-  if (ht == 128 && nc == 1) return qattn_mfma_start<128, 1, 2, 1, 3, bf16, bf16>(a, n_items, s);
-  if (ht == 256 && nc == 1) return qattn_mfma_start<256, 1, 2, 1, 1, bf16, bf16>(a, n_items, s);
+void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s) {
+  if (lds && ht == 64 && nc == 4) return qattn_lds_start<64, 1, 2, 4, 4, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 64 && nc == 2) return qattn_lds_start<64, 1, 2, 2, 5, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 64 && nc == 1) return qattn_lds_start<64, 1, 2, 1, 6, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 128 && nc == 2) return qattn_lds_start<128, 1, 2, 2, 4, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 128 && nc == 1) return qattn_lds_start<128, 1, 2, 1, 4, bf16, bf16>(a, n_items, s);
+  if (!lds && ht == 64 && nc == 4) return qattn_mfma_start<64, 1, 2, 4, 1, bf16, bf16>(a, n_items, s);
+  if (!lds && ht == 64 && nc == 2) return qattn_mfma_start<64, 1, 2, 2, 3, bf16, bf16>(a, n_items, s);
+  if (!lds && ht == 64 && nc == 1) return qattn_mfma_start<64, 1, 2, 1, 4, bf16, bf16>(a, n_items, s);
+  if (!lds && ht == 128 && nc == 2) return qattn_mfma_start<128, 1, 2, 2, 1, bf16, bf16>(a, n_items, s);
+  if (!lds && ht == 128 && nc == 1) return qattn_mfma_start<128, 1, 2, 1, 3, bf16, bf16>(a, n_items, s);
+  if (!lds && ht == 256 && nc == 1) return qattn_mfma_start<256, 1, 2, 1, 1, bf16, bf16>(a, n_items, s);
 }
 
 }  // namespace alora

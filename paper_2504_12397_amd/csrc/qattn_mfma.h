@@ -14,6 +14,7 @@
 // bits would add half of what the rounding of a bf16 result does), three for fp32.
 // The reference exponent of a column moves only when a score exceeds it by 2^8: almost no step rescales the sums.
 #pragma once
+#include "lds_dma.h"
 #include "qcache.h"
 
 namespace alora {
@@ -66,149 +67,112 @@ __device__ __forceinline__ float qa_sum4(float x) {
   return x + __shfl_xor(x, 32, 64);
 }
 
-// Any head size h <= HT that is a multiple of 8.  Channels from h on: the queries have zeros there and nothing is stored for them; what the lanes
-// read in their place (the next head's codes with this head's exponents) is a number where the head's own are.
-// DEPTH steps' codes are on the way at a time.
-template <int HT, int NQ, int NP, int NC, int DEPTH, typename TQ, typename T>
-__global__ __launch_bounds__(512, 2) void qattn_mfma_kernel(QAttnArgs a) {
-  constexpr int KS = HT / 32;       // products per block of 16 keys, dwords of K per lane
-  constexpr int CPL = HT / 16;      // channels of V per lane
-  constexpr int VB = CPL / 2;       // bytes of them
-  constexpr int VW = (VB + 3) / 4;
-  constexpr int KSC = HT == 256 ? 2 : 1;      // exponents of K per lane
-  extern __shared__ float s_join[];
-
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int j = lane & 15, kg = lane >> 4;
-  const QAttnItem it = a.items[blockIdx.x];
-  const int h = a.head_dim, hb = h / 2, nb = q_blocks(h);
-  const int G = a.n_q_heads / a.n_kv_heads;
-  const int hw = wave % a.hw, rest = wave / a.hw, sub = rest % a.kr, cg = rest / a.kr;
-  const int c_first = cg * 16 * NC, n_cols = min(it.n_cols - c_first, 16 * NC);      // columns of this wave, counted from c_first
-  const bool active = it.g0 + hw < a.n_kv_heads && n_cols > 0;
-  const int g = min(it.g0 + hw, a.n_kv_heads - 1);
-  const int col0 = it.col0 + c_first;
-
-  // keys of this wave: its share of those that its last column sees
-  const int last_tok = (col0 + max(n_cols, 1) - 1) / G, first_tok = col0 / G;
+// What a wave is to do, from its item and its place in the workgroup.
+struct QaWork {
+  int g, sub, cg, kr;            // kv head; share of the keys, group of columns
+  bool active, shared;
+  int col0, n_cols;              // its columns
+  int kbeg, kend, see_all;       // its keys; keys below see_all are seen by every column
+  int64_t key_row0;
+  int first_row, pos0, part;
+};
+template <int NC> __device__ __forceinline__ QaWork qa_work(const QAttnArgs &a, const QAttnItem &it, int wave) {
+  QaWork w;
+  const int G = a.n_q_heads / a.n_kv_heads, hw = wave % a.hw, rest = wave / a.hw;
+  w.sub = rest % a.kr; w.cg = rest / a.kr; w.kr = a.kr;
+  const int c_first = w.cg * 16 * NC;
+  w.n_cols = min(it.n_cols - c_first, 16 * NC);
+  w.active = it.g0 + hw < a.n_kv_heads && w.n_cols > 0;
+  w.g = min(it.g0 + hw, a.n_kv_heads - 1);
+  w.col0 = it.col0 + c_first;
+  w.shared = it.shared;
+  w.key_row0 = it.key_row0; w.first_row = it.first_row; w.pos0 = it.pos0; w.part = it.part;
+  const int last_tok = (w.col0 + max(w.n_cols, 1) - 1) / G, first_tok = w.col0 / G;
   int per = (it.kend - it.kbeg + a.kr - 1) / a.kr;
   per = (per + 31) & ~31;
-  const int kbeg = it.kbeg + sub * per;
-  int kend = min(it.kend, kbeg + per);
-  if (!it.shared) kend = min(kend, it.pos0 + last_tok + 1);
-  if (!active) kend = kbeg;
-  const int see_all = it.shared ? kend : min(kend, it.pos0 + first_tok + 1);      // keys below are seen by every column
+  w.kbeg = it.kbeg + w.sub * per;
+  w.kend = min(it.kend, w.kbeg + per);
+  if (!it.shared) w.kend = min(w.kend, it.pos0 + last_tok + 1);
+  if (!w.active) w.kend = w.kbeg;
+  w.see_all = it.shared ? w.kend : min(w.kend, it.pos0 + first_tok + 1);
+  return w;
+}
 
-  const int pitch = a.n_kv_heads * hb, spitch = a.n_kv_heads * nb;
-  const uint8_t *Kp = a.c.k + it.key_row0 * pitch + g * hb, *Vp = a.c.v + it.key_row0 * pitch + g * hb;
-  const uint8_t *Ksp = a.c.k_scale + it.key_row0 * spitch + g * nb, *Vsp = a.c.v_scale + it.key_row0 * spitch + g * nb;
-  const int ks_blk = min(kg * (HT / 4) / QBLOCK, nb - 1), vs_blk = min(CPL * j / QBLOCK, nb - 1);
-  const int k_off = j * pitch + kg * (HT / 8), v_off = 4 * kg * pitch + j * VB;
-  const int ks_off = j * spitch + ks_blk, vs_off = 4 * kg * spitch + vs_blk;
+// Codes and exponents of 32 keys, as the lanes hold them
+template <int HT> struct QaTile {
+  static constexpr int KS = HT / 32;                  // products per block of 16 keys, dwords of K per lane
+  static constexpr int CPL = HT / 16;                 // channels of V per lane ...
+  static constexpr int VB = CPL / 2;                  // ... and their bytes
+  static constexpr int VW = (VB + 3) / 4;
+  static constexpr int KSC = HT == 256 ? 2 : 1;       // exponents of K per lane
+  uint32_t k[2][KS];
+  uint32_t ks[2][KSC];
+  uint32_t v[2][4][VW];                               // [u][n]: key 16 u + 4 kg + n
+  uint32_t vs[2][4];
+};
 
-  // A step of 32 keys from k0 on, through a resource that ends with the wave's last key: keys beyond it read as zeros, without a branch.
-  struct Tile {
-    uint32_t k[2][KS];
-    uint32_t ks[2][KSC];
-    uint32_t v[2][4][VW];      // [u][n]: key 16 u + 4 kg + n
-    uint32_t vs[2][4];
-  };
-  auto rsrc = [&](const uint8_t *p, int k0, int row, int head) {
-    const int left = max(0, min(kend - k0, 32)) * row;
-    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (int64_t)k0 * row), (short)0, left > head ? left - head : 0, 0x00020000);
-  };
-  auto load_k = [&](Tile &t, int k0) {
-    const auto r = rsrc(Kp, k0, pitch, g * hb), rs = rsrc(Ksp, k0, spitch, g * nb);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if constexpr (KS == 2) {
-        const auto w = __builtin_amdgcn_raw_buffer_load_b64(r, k_off, 16 * u * pitch, 0);
-        t.k[u][0] = w[0]; t.k[u][1] = w[1];
-      } else {
-#pragma unroll
-        for (int d = 0; d < KS; d += 4) {
-          const auto w = __builtin_amdgcn_raw_buffer_load_b128(r, k_off + 4 * d, 16 * u * pitch, 0);
-          t.k[u][d] = w[0]; t.k[u][d + 1] = w[1]; t.k[u][d + 2] = w[2]; t.k[u][d + 3] = w[3];
-        }
-      }
-      t.ks[u][0] = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off, 16 * u * spitch, 0);
-      if constexpr (KSC == 2) t.ks[u][1] = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off + (ks_blk + 1 < nb ? 1 : 0), 16 * u * spitch, 0);
-    }
-  };
-  auto load_v = [&](Tile &t, int k0) {
-    const auto r = rsrc(Vp, k0, pitch, g * hb), rs = rsrc(Vsp, k0, spitch, g * nb);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        if constexpr (VB == 2) {
-          t.v[u][n][0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, v_off, (16 * u + n) * pitch, 0);
-        } else if constexpr (VB == 4) {
-          t.v[u][n][0] = __builtin_amdgcn_raw_buffer_load_b32(r, v_off, (16 * u + n) * pitch, 0);
-        } else {
-          const auto w = __builtin_amdgcn_raw_buffer_load_b64(r, v_off, (16 * u + n) * pitch, 0);
-          t.v[u][n][0] = w[0]; t.v[u][n][1] = w[1];
-        }
-        t.vs[u][n] = __builtin_amdgcn_raw_buffer_load_b8(rs, vs_off, (16 * u + n) * spitch, 0);
-      }
-  };
-
-  Tile ring[DEPTH];
-#pragma unroll
-  for (int d = 0; d < DEPTH; ++d) { load_k(ring[d], kbeg + 32 * d); load_v(ring[d], kbeg + 32 * d); }
-
-  // queries
+// The columns of a wave: queries, running sums, and what is done with 32 keys.
+template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColumns {
+  typedef QaTile<HT> Tile;
+  static constexpr int KS = Tile::KS, CPL = Tile::CPL, VW = Tile::VW, KSC = Tile::KSC;
   uint32_t qf[NC][NQ][KS][4];
-  int lim[NC];      // last key that the column sees
-#pragma unroll
-  for (int nc = 0; nc < NC; ++nc) {
-    const int c = 16 * nc + j, tok = (col0 + c) / G, hj = col0 + c - tok * G;
-    const bool there = active && c < n_cols;
-    lim[nc] = it.shared || !there ? 0x7fffffff : it.pos0 + tok;
-    const int row = !there ? 0 : it.shared ? a.rows[it.first_row + tok] : it.first_row + tok;
-    const TQ *q = (const TQ *)a.Q + ((int64_t)row * a.n_q_heads + g * G + (there ? hj : 0)) * h;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int ch = kg * (HT / 4) + 8 * s;
-      const bool in = there && ch < h;
-      if constexpr (sizeof(TQ) == 2 && NQ == 1) {
-        const qa_u32x4 w = in ? *reinterpret_cast<const qa_u32x4 *>(q + ch) : qa_u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) qf[nc][0][s][i] = w[i];
-      } else {
-        float x[8];
-        if constexpr (sizeof(TQ) == 2) {
-          typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-          f16x8_t w = {};
-          if (in) w = *reinterpret_cast<const f16x8_t *>(q + ch);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = (float)w[i];
-        } else {
-          qa_f32x4 w0 = {}, w1 = {};
-          if (in) { w0 = *reinterpret_cast<const qa_f32x4 *>(q + ch); w1 = *reinterpret_cast<const qa_f32x4 *>(q + ch + 4); }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) { x[i] = w0[i]; x[4 + i] = w1[i]; }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) qa_split<NQ>(x[2 * i], x[2 * i + 1], &qf[nc][0][s][i], KS * 4);
-      }
-    }
-  }
-
-  qa_f32x4 o[NC][CPL];
+  int lim[NC];                            // last key that the column sees
+  qa_f32x4 o[NC][CPL];                    // o[c][v] of lane (j, kg): channel CPL * (4 kg + v) + c of column j
   float m_ref[NC], neg_m[NC], l[NC];      // reference exponent (log2), its negative or 0 where there is none, this lane's part of the sum
   uint32_t nan_blocks[NC];                // blocks of 32 channels in which the column has met a value that is not a number
-#pragma unroll
-  for (int nc = 0; nc < NC; ++nc) {
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) o[nc][c] = qa_f32x4{0.f, 0.f, 0.f, 0.f};
-    m_ref[nc] = -INFINITY;
-    neg_m[nc] = l[nc] = 0.f;
-    nan_blocks[nc] = 0;
-  }
-  const float c_scale = a.sm_scale * 1.4426950408889634f;
+  int j, kg;
+  float c_scale;
 
-  auto step = [&](Tile &t, int k0) {
+  __device__ __forceinline__ int row_of(const QAttnArgs &a, const QaWork &w, int tok) const { return w.shared ? a.rows[w.first_row + tok] : w.first_row + tok; }
+
+  __device__ __forceinline__ void begin(const QAttnArgs &a, const QaWork &w, int lane) {
+    j = lane & 15; kg = lane >> 4;
+    c_scale = a.sm_scale * 1.4426950408889634f;
+    const int G = a.n_q_heads / a.n_kv_heads, h = a.head_dim;
+#pragma unroll
+    for (int nc = 0; nc < NC; ++nc) {
+      const int c = 16 * nc + j, tok = (w.col0 + c) / G, hj = w.col0 + c - tok * G;
+      const bool there = w.active && c < w.n_cols;
+      lim[nc] = w.shared || !there ? 0x7fffffff : w.pos0 + tok;
+      const int row = there ? row_of(a, w, tok) : 0;
+      const TQ *q = (const TQ *)a.Q + ((int64_t)row * a.n_q_heads + w.g * G + (there ? hj : 0)) * h;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int ch = kg * (HT / 4) + 8 * s;
+        const bool in = there && ch < h;
+        if constexpr (sizeof(TQ) == 2 && NQ == 1) {
+          const qa_u32x4 x = in ? *reinterpret_cast<const qa_u32x4 *>(q + ch) : qa_u32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) qf[nc][0][s][i] = x[i];
+        } else {
+          float x[8];
+          if constexpr (sizeof(TQ) == 2) {
+            typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+            f16x8_t y = {};
+            if (in) y = *reinterpret_cast<const f16x8_t *>(q + ch);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (float)y[i];
+          } else {
+            qa_f32x4 y0 = {}, y1 = {};
+            if (in) { y0 = *reinterpret_cast<const qa_f32x4 *>(q + ch); y1 = *reinterpret_cast<const qa_f32x4 *>(q + ch + 4); }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { x[i] = y0[i]; x[4 + i] = y1[i]; }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) qa_split<NQ>(x[2 * i], x[2 * i + 1], &qf[nc][0][s][i], KS * 4);
+        }
+      }
+#pragma unroll
+      for (int c2 = 0; c2 < CPL; ++c2) o[nc][c2] = qa_f32x4{0.f, 0.f, 0.f, 0.f};
+      m_ref[nc] = -INFINITY;
+      neg_m[nc] = l[nc] = 0.f;
+      nan_blocks[nc] = 0;
+    }
+  }
+
+  // 32 keys from k0 on.  k_used() is called once t.k has been read, need_v() before t.v is, v_used() after.
+  template <typename KU, typename NV, typename VU>
+  __device__ __forceinline__ void step(const QAttnArgs &a, const QaWork &w, Tile &t, int k0, KU k_used, NV need_v, VU v_used) {
     qa_f32x4 sc[NC][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -217,8 +181,8 @@ __global__ __launch_bounds__(512, 2) void qattn_mfma_kernel(QAttnArgs a) {
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const float e = qa_scale(t.ks[u][KSC == 2 ? s / 4 : 0]);
-        const uint32_t w = t.k[u][s];
-        const qa_u32x4 kf = {qa_pair(w, e, 0), qa_pair(w, e, 1), qa_pair(w, e, 2), qa_pair(w, e, 3)};
+        const uint32_t c = t.k[u][s];
+        const qa_u32x4 kf = {qa_pair(c, e, 0), qa_pair(c, e, 1), qa_pair(c, e, 2), qa_pair(c, e, 3)};
 #pragma unroll
         for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
@@ -228,8 +192,9 @@ __global__ __launch_bounds__(512, 2) void qattn_mfma_kernel(QAttnArgs a) {
           }
       }
     }
-    load_k(t, k0 + 32 * DEPTH);      // (each half of the tile is asked for again as soon as it has been used)
-    if (k0 + 32 > see_all) {      // a step that some column sees in part
+    k_used();
+    need_v();
+    if (k0 + 32 > w.see_all) {      // a step that some column sees in part
       bool bad = false;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -239,21 +204,23 @@ __global__ __launch_bounds__(512, 2) void qattn_mfma_kernel(QAttnArgs a) {
           bad |= t.vs[u][v] == (uint32_t)Q_E_NAN;
 #pragma unroll
           for (int nc = 0; nc < NC; ++nc)
-            if (key >= kend || key > lim[nc]) sc[nc][u][v] = -INFINITY;
+            if (key >= w.kend || key > lim[nc]) sc[nc][u][v] = -INFINITY;
         }
       if (__any(bad)) {
         // 0 times NaN would reach the columns that do not see the key: its values count as 0, and the columns that do see it remember the block
+        const int nb = q_blocks(a.head_dim);
+        const uint8_t *scales = a.c.v_scale + (w.key_row0 * a.n_kv_heads + w.g) * nb;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             const int key = k0 + 16 * u + 4 * kg + v;
-            const uint8_t *sp = Vsp + (int64_t)min(key, kend - 1) * spitch;
+            const uint8_t *sp = scales + (int64_t)min(key, w.kend - 1) * a.n_kv_heads * nb;
             uint32_t blocks = 0;
             for (int b = 0; b < nb; ++b) blocks |= (sp[b] == Q_E_NAN ? 1u : 0u) << b;
 #pragma unroll
             for (int nc = 0; nc < NC; ++nc)
-              if (key < kend && key <= lim[nc]) nan_blocks[nc] |= blocks;
+              if (key < w.kend && key <= lim[nc]) nan_blocks[nc] |= blocks;
             if (t.vs[u][v] == (uint32_t)Q_E_NAN) {
               t.vs[u][v] = 127;
 #pragma unroll
@@ -293,10 +260,10 @@ __global__ __launch_bounds__(512, 2) void qattn_mfma_kernel(QAttnArgs a) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) ev[u][n] = qa_scale(t.vs[u][n]);
 #pragma unroll
-    for (int w = 0; w < CPL / 2; ++w) {
-      uint32_t e[8];      // channels 2 w and 2 w + 1 of the lane's eight keys
+    for (int c2 = 0; c2 < CPL / 2; ++c2) {
+      uint32_t e[8];      // channels 2 c2 and 2 c2 + 1 of the lane's eight keys
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = qa_pair(t.v[i >> 2][i & 3][w / 4], ev[i >> 2][i & 3], w & 3);
+      for (int i = 0; i < 8; ++i) e[i] = qa_pair(t.v[i >> 2][i & 3][c2 / 4], ev[i >> 2][i & 3], c2 & 3);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const uint32_t sel = half ? 0x07060302u : 0x05040100u;
@@ -308,25 +275,20 @@ __global__ __launch_bounds__(512, 2) void qattn_mfma_kernel(QAttnArgs a) {
 #pragma unroll
           for (int p = 0; p < NP; ++p) {
             const qa_u32x4 pv = {pf[nc][p][0], pf[nc][p][1], pf[nc][p][2], pf[nc][p][3]};
-            o[nc][2 * w + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(qa_bf16x8, vf), __builtin_bit_cast(qa_bf16x8, pv), o[nc][2 * w + half], 0, 0, 0);
+            o[nc][2 * c2 + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(qa_bf16x8, vf), __builtin_bit_cast(qa_bf16x8, pv), o[nc][2 * c2 + half], 0, 0, 0);
           }
       }
     }
-    load_v(t, k0 + 32 * DEPTH);
-  };
-  for (int k0 = kbeg; k0 < kend; k0 += 32 * DEPTH) {
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d)
-      if (k0 + 32 * d < kend) step(ring[d], k0 + 32 * d);
+    v_used();
   }
 
-  // ---- join the waves that share a head's keys, in pairs: the upper half of those left hands its sums to the lower half
-  if (a.kr > 1) {
-    constexpr int REGS = NC * (CPL * 4 + 3);
+  // joins the waves that share a head's keys, in pairs: the upper half of those left hands its sums to the lower half.  All waves of the workgroup call this.
+  static constexpr int REGS = NC * (CPL * 4 + 3);
+  __device__ __forceinline__ void join(const QAttnArgs &a, const QaWork &w, int hw, int lane, float *s_join) {
     for (int left = a.kr; left > 1; left >>= 1) {
       const int to = left >> 1;
-      float *slot = s_join + (size_t)((cg * to + (sub & (to - 1))) * a.hw + hw) * REGS * 64 + lane;
-      if (sub >= to && sub < left) {
+      float *slot = s_join + (size_t)((w.cg * to + (w.sub & (to - 1))) * a.hw + hw) * REGS * 64 + lane;
+      if (w.sub >= to && w.sub < left) {
         int r = 0;
 #pragma unroll
         for (int nc = 0; nc < NC; ++nc) {
@@ -340,7 +302,7 @@ __global__ __launch_bounds__(512, 2) void qattn_mfma_kernel(QAttnArgs a) {
         }
       }
       __syncthreads();
-      if (sub < to) {
+      if (w.sub < to) {
 #pragma unroll
         for (int nc = 0; nc < NC; ++nc) {
           const float *from = slot + 64 * nc * (CPL * 4 + 3);
@@ -359,63 +321,263 @@ __global__ __launch_bounds__(512, 2) void qattn_mfma_kernel(QAttnArgs a) {
       }
       __syncthreads();
     }
-    if (sub != 0) return;
   }
 
-  // ---- o[c][v] of lane (j, kg) is channel CPL * (4 kg + v) + c of column j
+  // the result, or the partial record
+  __device__ __forceinline__ void finish(const QAttnArgs &a, const QaWork &w) {
+    const int G = a.n_q_heads / a.n_kv_heads, h = a.head_dim;
 #pragma unroll
-  for (int nc = 0; nc < NC; ++nc) {
-    const float l_tot = qa_sum4(l[nc]);
-    uint32_t bad = nan_blocks[nc];
-    bad |= __shfl_xor(bad, 16, 64);
-    bad |= __shfl_xor(bad, 32, 64);
-    const int c = 16 * nc + j;
-    if (!active || c >= n_cols) continue;
-    const int tok = (col0 + c) / G, hj = col0 + c - tok * G;
-    const int row = it.shared ? a.rows[it.first_row + tok] : it.first_row + tok;
-    const int64_t rh = (int64_t)row * a.n_q_heads + g * G + hj;
-    const bool direct = a.out != nullptr;
-    const float inv = direct ? 1.0f / l_tot : 1.0f;
-    float *rec = direct ? nullptr : a.partials + (rh * a.n_parts + it.part) * (h + 2);
+    for (int nc = 0; nc < NC; ++nc) {
+      const float l_tot = qa_sum4(l[nc]);
+      uint32_t bad = nan_blocks[nc];
+      bad |= __shfl_xor(bad, 16, 64);
+      bad |= __shfl_xor(bad, 32, 64);
+      const int c = 16 * nc + j;
+      if (!w.active || c >= w.n_cols) continue;
+      const int tok = (w.col0 + c) / G, hj = w.col0 + c - tok * G;
+      const int64_t rh = (int64_t)row_of(a, w, tok) * a.n_q_heads + w.g * G + hj;
+      const bool direct = a.out != nullptr;
+      const float inv = direct ? 1.0f / l_tot : 1.0f;
+      float *rec = direct ? nullptr : a.partials + (rh * a.n_parts + w.part) * (h + 2);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      constexpr int PIECE = CPL < 8 ? CPL : 8;
+      for (int v = 0; v < 4; ++v) {
+        constexpr int PIECE = CPL < 8 ? CPL : 8;
 #pragma unroll
-      for (int c0 = 0; c0 < CPL; c0 += PIECE) {
-        const int ch = CPL * (4 * kg + v) + c0;
-        if (ch >= h) continue;
-        const float nan = (bad >> (ch / QBLOCK)) & 1 ? __builtin_nanf("") : 0.f;
-        float x[PIECE];
+        for (int c0 = 0; c0 < CPL; c0 += PIECE) {
+          const int ch = CPL * (4 * kg + v) + c0;
+          if (ch >= h) continue;
+          const float nan = (bad >> (ch / QBLOCK)) & 1 ? __builtin_nanf("") : 0.f;
+          float x[PIECE];
 #pragma unroll
-        for (int i = 0; i < PIECE; ++i) x[i] = o[nc][c0 + i][v] * inv + nan;
-        if (!direct) {
+          for (int i = 0; i < PIECE; ++i) x[i] = o[nc][c0 + i][v] * inv + nan;
+          if (!direct) {
 #pragma unroll
-          for (int i = 0; i < PIECE; i += 2) *reinterpret_cast<float2 *>(rec + ch + i) = make_float2(x[i], x[i + 1]);
-        } else if constexpr (sizeof(T) == 2) {
-          uint32_t w[PIECE / 2];
+            for (int i = 0; i < PIECE; i += 2) *reinterpret_cast<float2 *>(rec + ch + i) = make_float2(x[i], x[i + 1]);
+          } else if constexpr (sizeof(T) == 2) {
+            uint32_t y[PIECE / 2];
 #pragma unroll
-          for (int i = 0; i < PIECE / 2; ++i) w[i] = qa_pack(x[2 * i], x[2 * i + 1]);
-          T *out = (T *)a.out + rh * h + ch;
-          if constexpr (PIECE == 8) *reinterpret_cast<uint4 *>(out) = uint4{w[0], w[1], w[2], w[3]};
-          else *reinterpret_cast<uint2 *>(out) = uint2{w[0], w[1]};
-        } else {
-          T *out = (T *)a.out + rh * h + ch;
+            for (int i = 0; i < PIECE / 2; ++i) y[i] = qa_pack(x[2 * i], x[2 * i + 1]);
+            T *out = (T *)a.out + rh * h + ch;
+            if constexpr (PIECE == 8) *reinterpret_cast<uint4 *>(out) = uint4{y[0], y[1], y[2], y[3]};
+            else *reinterpret_cast<uint2 *>(out) = uint2{y[0], y[1]};
+          } else {
+            T *out = (T *)a.out + rh * h + ch;
 #pragma unroll
-          for (int i = 0; i < PIECE; i += 4) *reinterpret_cast<float4 *>(out + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+            for (int i = 0; i < PIECE; i += 4) *reinterpret_cast<float4 *>(out + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+          }
         }
       }
-    }
-    if (!direct && kg == 0) {
-      rec[h] = m_ref[nc] == -INFINITY ? (l_tot == 0.f ? -INFINITY : 0.f) : m_ref[nc] * 0.6931471805599453f;      // (NaN scores have no maximum, and have to count)
-      rec[h + 1] = l_tot;
+      if (!direct && kg == 0) {
+        rec[h] = m_ref[nc] == -INFINITY ? (l_tot == 0.f ? -INFINITY : 0.f) : m_ref[nc] * 0.6931471805599453f;      // (NaN scores have no maximum, and have to count)
+        rec[h + 1] = l_tot;
+      }
     }
   }
+};
+
+// Any head size h <= HT that is a multiple of 8; codes wait in registers.  Channels from h on: the queries have zeros there and nothing is stored for
+// them; what the lanes read in their place (the next head's codes with this head's exponents) is a number where the head's own are.
+// DEPTH steps' codes are on the way at a time.
+template <int HT, int NQ, int NP, int NC, int DEPTH, typename TQ, typename T>
+__global__ __launch_bounds__(64 * qattn_waves(HT), HT == 256 ? 1 : 2) void qattn_mfma_kernel(QAttnArgs a) {
+  typedef QaTile<HT> Tile;
+  extern __shared__ float s_join[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = lane & 15, kg = lane >> 4;
+  const QaWork w = qa_work<NC>(a, a.items[blockIdx.x], wave);
+  const int hb = a.head_dim / 2, nb = q_blocks(a.head_dim), g = w.g;
+  const int pitch = a.n_kv_heads * hb, spitch = a.n_kv_heads * nb;
+  const uint8_t *Kp = a.c.k + w.key_row0 * pitch + g * hb, *Vp = a.c.v + w.key_row0 * pitch + g * hb;
+  const uint8_t *Ksp = a.c.k_scale + w.key_row0 * spitch + g * nb, *Vsp = a.c.v_scale + w.key_row0 * spitch + g * nb;
+  const int ks_blk = min(kg * (HT / 4) / QBLOCK, nb - 1), vs_blk = min(Tile::CPL * j / QBLOCK, nb - 1);
+  const int k_off = j * pitch + kg * (HT / 8), v_off = 4 * kg * pitch + j * Tile::VB;
+  const int ks_off = j * spitch + ks_blk, vs_off = 4 * kg * spitch + vs_blk;
+
+  // Through a resource that ends with the wave's last key: keys beyond it read as zeros, without a branch.
+  auto rsrc = [&](const uint8_t *p, int k0, int row, int head) {
+    const int left = max(0, min(w.kend - k0, 32)) * row;
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (int64_t)k0 * row), (short)0, left > head ? left - head : 0, 0x00020000);
+  };
+  auto load_k = [&](Tile &t, int k0) {
+    const auto r = rsrc(Kp, k0, pitch, g * hb), rs = rsrc(Ksp, k0, spitch, g * nb);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (Tile::KS == 2) {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, k_off, 16 * u * pitch, 0);
+        t.k[u][0] = x[0]; t.k[u][1] = x[1];
+      } else {
+#pragma unroll
+        for (int d = 0; d < Tile::KS; d += 4) {
+          const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, k_off + 4 * d, 16 * u * pitch, 0);
+          t.k[u][d] = x[0]; t.k[u][d + 1] = x[1]; t.k[u][d + 2] = x[2]; t.k[u][d + 3] = x[3];
+        }
+      }
+      t.ks[u][0] = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off, 16 * u * spitch, 0);
+      if constexpr (Tile::KSC == 2) t.ks[u][1] = __builtin_amdgcn_raw_buffer_load_b8(rs, ks_off + (ks_blk + 1 < nb ? 1 : 0), 16 * u * spitch, 0);
+    }
+  };
+  auto load_v = [&](Tile &t, int k0) {
+    const auto r = rsrc(Vp, k0, pitch, g * hb), rs = rsrc(Vsp, k0, spitch, g * nb);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        if constexpr (Tile::VB == 2) {
+          t.v[u][n][0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, v_off, (16 * u + n) * pitch, 0);
+        } else if constexpr (Tile::VB == 4) {
+          t.v[u][n][0] = __builtin_amdgcn_raw_buffer_load_b32(r, v_off, (16 * u + n) * pitch, 0);
+        } else {
+          const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, v_off, (16 * u + n) * pitch, 0);
+          t.v[u][n][0] = x[0]; t.v[u][n][1] = x[1];
+        }
+        t.vs[u][n] = __builtin_amdgcn_raw_buffer_load_b8(rs, vs_off, (16 * u + n) * spitch, 0);
+      }
+  };
+
+  Tile ring[DEPTH];
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) { load_k(ring[d], w.kbeg + 32 * d); load_v(ring[d], w.kbeg + 32 * d); }
+  QaColumns<HT, NQ, NP, NC, TQ, T> q;
+  q.begin(a, w, lane);
+  for (int k0 = w.kbeg; k0 < w.kend; k0 += 32 * DEPTH) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {      // each half of a tile is asked for again as soon as it has been used
+      const int at = k0 + 32 * d;
+      if (at < w.kend) q.step(a, w, ring[d], at, [&] { load_k(ring[d], at + 32 * DEPTH); }, [] {}, [&] { load_v(ring[d], at + 32 * DEPTH); });
+    }
+  }
+  if (a.kr > 1) {
+    q.join(a, w, wave % a.hw, lane, s_join);
+    if (w.sub != 0) return;
+  }
+  q.finish(a, w);
+}
+
+// Head sizes 64 and 128 whose codes begin at multiples of 16 bytes: codes and exponents go from memory into LDS, in whole 16-byte pieces of
+// a head's row, each wave into a ring of its own (no barriers), and from there into registers.  A request of 64 lanes keeps the vector memory unit busy for
+// about 16 clocks whatever its lanes ask for: six of them a step instead of twenty.  Rows of V lie in LDS in the order that gives the four lanes
+// (j, 0..3) of a read different banks; pieces of K are turned by a place every four rows for the same reason.
+template <int HT, int DEPTH> struct QaRing {
+  static constexpr int RB = HT / 2, ROWS = 32 * RB, STAGE = 2 * ROWS + 512, WAVE = DEPTH * STAGE;      // bytes: a row, 32 of them, a step, a wave's ring
+  static constexpr int REQ = RB / 32, PER_STEP = 2 * REQ + 2;                                         // requests of an array and of a step
+};
+__device__ __forceinline__ void qa_dword_to_lds(i32x4 rsrc, int voff, int lds) {
+  lds = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
+}
+template <int HT, int NQ, int NP, int NC, int DEPTH, typename TQ, typename T>
+__global__ __launch_bounds__(512, 2) void qattn_lds_kernel(QAttnArgs a) {
+  typedef QaTile<HT> Tile;
+  typedef QaRing<HT, DEPTH> R;
+  extern __shared__ __align__(16) char s_ring[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = lane & 15, kg = lane >> 4;
+  const QaWork w = qa_work<NC>(a, a.items[blockIdx.x], wave);
+  constexpr int hb = HT / 2, nb = HT / QBLOCK;
+  const int pitch = a.n_kv_heads * hb, spitch = a.n_kv_heads * nb, g = w.g;
+  const uint8_t *Kp = a.c.k + w.key_row0 * pitch + g * hb, *Vp = a.c.v + w.key_row0 * pitch + g * hb;
+  // exponents come as the dword that holds a head's (two heads share one at HT = 64)
+  const int e_at = g * nb & ~3, e_in = g * nb & 3;
+  const uint8_t *Ksp = a.c.k_scale + w.key_row0 * spitch + e_at, *Vsp = a.c.v_scale + w.key_row0 * spitch + e_at;
+
+  // lane i of a request: place i of 64 pieces of 16 bytes
+  constexpr int PIECES = hb / 16, RPR = 64 / PIECES;      // pieces of a row, rows of a request
+  const int slot_row = lane / PIECES, piece = lane % PIECES;
+  int k_voff, v_voff;
+  if constexpr (HT == 128) {
+    k_voff = slot_row * pitch + ((piece - (slot_row >> 2)) & 3) * 16;
+    v_voff = (4 * (slot_row & 3) + (slot_row >> 2)) * pitch + piece * 16;
+  } else {
+    k_voff = slot_row * pitch + ((piece - (slot_row >> 3)) & 1) * 16;
+    v_voff = ((slot_row & 16) + 4 * (slot_row & 3) + ((slot_row & 15) >> 2)) * pitch + piece * 16;
+  }
+  const int e_voff = lane < 32 ? lane * spitch : (int)0x80000000;      // (the upper lanes ask for nothing)
+  char *ring = s_ring + wave * R::WAVE;
+  const int lds0 = (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)ring;
+  auto ask = [&](int k0, int slot) {
+    const int left = max(0, min(w.kend - k0, 32)), rows = left * pitch - g * hb, exps = left * spitch - e_at;
+    const i32x4 rk = make_rsrc(Kp + (int64_t)k0 * pitch, left > 0 ? rows : 0), rv = make_rsrc(Vp + (int64_t)k0 * pitch, left > 0 ? rows : 0);
+    const i32x4 ek = make_rsrc(Ksp + (int64_t)k0 * spitch, left > 0 ? exps : 0), ev = make_rsrc(Vsp + (int64_t)k0 * spitch, left > 0 ? exps : 0);
+    const int to = lds0 + slot * R::STAGE;
+#pragma unroll
+    for (int i = 0; i < R::REQ; ++i) load_to_lds(rk, k_voff, i * RPR * pitch, to + i * 1024);
+    qa_dword_to_lds(ek, e_voff, to + 2 * R::ROWS);
+#pragma unroll
+    for (int i = 0; i < R::REQ; ++i) load_to_lds(rv, v_voff, i * RPR * pitch, to + R::ROWS + i * 1024);
+    qa_dword_to_lds(ev, e_voff, to + 2 * R::ROWS + 256);
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) ask(w.kbeg + 32 * d, d);
+  QaColumns<HT, NQ, NP, NC, TQ, T> q;
+  q.begin(a, w, lane);
+  // the queries are here before the first step (a wait for them inside the loop would be one for everything on the way)
+#pragma unroll
+  for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+    for (int p = 0; p < NQ; ++p)
+#pragma unroll
+      for (int s = 0; s < Tile::KS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(q.qf[nc][p][s][i]));
+
+  const int k_at = HT == 128 ? j * hb + ((kg + (j >> 2)) & 3) * 16 : j * hb + (((kg >> 1) + (j >> 3)) & 1) * 16 + (kg & 1) * 8;
+  const int ks_at = 2 * R::ROWS + 4 * j + e_in + kg * (HT / 4) / QBLOCK;
+  const int v_at = R::ROWS + kg * hb + j * Tile::VB;      // slot of row 16 u + 4 kg + n: 16 u + 4 n + kg
+  const int vs_at = 2 * R::ROWS + 256 + 16 * kg + e_in + Tile::CPL * j / QBLOCK;
+  int slot = 0;
+  for (int k0 = w.kbeg; k0 < w.kend; k0 += 32) {
+    wait_vm<(DEPTH - 1) * R::PER_STEP>();
+    const char *st = ring + slot * R::STAGE;
+    Tile t;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (HT == 128) {
+        const qa_u32x4 x = *reinterpret_cast<const qa_u32x4 *>(st + k_at + u * 16 * hb);
+        t.k[u][0] = x[0]; t.k[u][1] = x[1]; t.k[u][2] = x[2]; t.k[u][3] = x[3];
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2 *>(st + k_at + u * 16 * hb);
+        t.k[u][0] = x.x; t.k[u][1] = x.y;
+      }
+      t.ks[u][0] = (uint8_t)st[ks_at + 64 * u];
+    }
+    auto need_v = [&] {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          if constexpr (HT == 128) t.v[u][n][0] = *reinterpret_cast<const uint32_t *>(st + v_at + (16 * u + 4 * n) * hb);
+          else t.v[u][n][0] = *reinterpret_cast<const uint16_t *>(st + v_at + (16 * u + 4 * n) * hb);
+          t.vs[u][n] = (uint8_t)st[vs_at + 64 * u + 4 * n];
+        }
+      wait_lds();      // the step has left its place in the ring
+      ask(k0 + 32 * DEPTH, slot);
+    };
+    q.step(a, w, t, k0, [] {}, need_v, [] {});
+    slot = slot + 1 == DEPTH ? 0 : slot + 1;
+  }
+  wait_vm<0>();      // (nothing of this wave may land in LDS that is another's by then)
+  if (a.kr > 1) {
+    __syncthreads();
+    q.join(a, w, wave % a.hw, lane, reinterpret_cast<float *>(s_ring));
+    if (w.sub != 0) return;
+  }
+  q.finish(a, w);
 }
 
 template <int HT, int NQ, int NP, int NC, int DEPTH, typename TQ, typename T>
 void qattn_mfma_start(const QAttnArgs &a, int n_items, hipStream_t s) {
   auto kern = qattn_mfma_kernel<HT, NQ, NP, NC, DEPTH, TQ, T>;
-  const size_t smem = a.kr == 1 ? 0 : (size_t)4 * NC * (HT / 4 + 3) * 64 * sizeof(float);      // four waves hand over at most
+  constexpr int W = qattn_waves(HT);
+  const size_t smem = a.kr == 1 ? 0 : (size_t)(W / 2) * NC * (HT / 4 + 3) * 64 * sizeof(float);      // half of the waves hand over at most
+  if (smem > 48 * 1024) (void)hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  hipLaunchKernelGGL(kern, dim3(n_items), dim3(64 * W), smem, s, a);
+}
+template <int HT, int NQ, int NP, int NC, int DEPTH, typename TQ, typename T>
+void qattn_lds_start(const QAttnArgs &a, int n_items, hipStream_t s) {
+  auto kern = qattn_lds_kernel<HT, NQ, NP, NC, DEPTH, TQ, T>;
+  const size_t join = a.kr == 1 ? 0 : (size_t)4 * NC * (HT / 4 + 3) * 64 * sizeof(float), ring = (size_t)8 * QaRing<HT, DEPTH>::WAVE;
+  const size_t smem = join > ring ? join : ring;
+  static_assert(8 * QaRing<HT, DEPTH>::WAVE <= 160 * 1024 && 4 * NC * (HT / 4 + 3) * 256 <= 160 * 1024, "");
   if (smem > 48 * 1024) (void)hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   hipLaunchKernelGGL(kern, dim3(n_items), dim3(512), smem, s, a);
 }

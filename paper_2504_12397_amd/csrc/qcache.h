@@ -47,8 +47,10 @@ template <typename T>
 void launch_qattn_plain(const void *Q, QueryType qt, const QRows &c, const SeqMeta *seqs, const int32_t *row_seq, const LayerDims &L, int T_rows,
                         int n_splits, float *partials, T *out, hipStream_t s);
 
-// Head sizes that are multiples of 8, on the matrix units.  A workgroup of eight waves is hw kv heads x kr shares of the item's keys x cw
+// Head sizes that are multiples of 8, on the matrix units.  A workgroup of eight waves (four for heads of more than 128 channels, whose sums and
+// queries take more registers than a wave of eight may have) is hw kv heads x kr shares of the item's keys x cw
 // groups of 16 * nc columns; a column is a (row, query head) pair: column c of a unit is head c % G of its row c / G.
+__host__ __device__ constexpr int qattn_waves(int ht) { return ht == 256 ? 4 : 8; }
 struct QAttnItem {
   int64_t key_row0;         // pool row of key 0
   int32_t kbeg, kend;       // keys, counted from key_row0; none beyond kend is read
@@ -72,8 +74,9 @@ struct QAttnArgs {
   void *out;                // [T, n_q_heads, head_dim], with n_parts == 1 only
 };
 // ht: 64, 128 or 256, the smallest that holds head_dim.  Codes begin at multiples of 4 bytes, queries and results of 16.
-void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, hipStream_t s);      // queries of bf16; nc 1, 2 or 4 (ht 256: 1, 2)
-void launch_qattn_mfma_f16(const QAttnArgs &a, int n_items, int ht, int nc, hipStream_t s);       // of fp16; nc 1 or 2 (ht 256: 1)
-void launch_qattn_mfma_f32(const QAttnArgs &a, int n_items, int ht, int nc, hipStream_t s);       // of fp32; nc 1
+// lds: head_dim is 64 (with an even number of kv heads) or 128, codes begin at multiples of 16 bytes and exponents at multiples of 4.
+void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s);      // queries of bf16; nc 1, 2 or 4 (ht 256: 1, 2)
+void launch_qattn_mfma_f16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s);       // of fp16; nc 1 or 2 (ht 256: 1)
+void launch_qattn_mfma_f32(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s);       // of fp32; nc 1
 
 }  // namespace alora
