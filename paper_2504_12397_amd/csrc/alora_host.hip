@@ -1424,8 +1424,11 @@ bool cut_ranges(std::vector<RowRange> &ranges, int chunk_rows, int64_t *n_chunks
   *n_chunks = n;
   return n <= 0x7fffffff;
 }
-// Rows of a piece: about 32 KB of the widest array
-int chunk_rows_of(int64_t row_bytes) { return (int)std::max<int64_t>(1, std::min<int64_t>(4096, 32768 / std::max<int64_t>(row_bytes, 1))); }
+// Rows of a piece: 4 to 32 KB of the widest array, 2048 workgroups where the call has that much
+int chunk_rows_of(int64_t row_bytes, int64_t rows, int64_t planes) {
+  const int64_t b = std::min<int64_t>(32768, std::max<int64_t>(4096, rows * planes * row_bytes / 2048));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(4096, b / std::max<int64_t>(row_bytes, 1)));
+}
 
 // One launch over ranges x planes: `launch` gets the arguments.
 template <typename F>
@@ -1495,7 +1498,7 @@ alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int
   if (job.ranges.empty()) return ALORA_OK;
   if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
   HIP_TRY(ctx, hipSetDevice(ctx->device));
-  const int chunk = chunk_rows_of(widest);
+  const int chunk = chunk_rows_of(widest, job.rows, (int64_t)arrays.size());
   auto copy = [&](const std::vector<RowRange> &r, const std::vector<RowPlane> &planes) {
     return move_rows(ctx, r, planes, chunk, s, [&](const RowsArgs &a, const RowsFew &few) { launch_rows_copy(a, few, s); });
   };
@@ -1576,10 +1579,10 @@ alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_di
   for (int l = 0; l < n_layers; ++l)
     for (int v = 0; v < 2; ++v) {
       void *f = v ? full[l].v : full[l].k, *q = v ? four[l].v : four[l].k, *e = v ? four[l].v_scale : four[l].k_scale;
-      wide = wide && (((uintptr_t)f | (uintptr_t)q) % 16 == 0);
+      wide = wide && (uintptr_t)f % 16 == 0 && (uintptr_t)q % 4 == 0;
       planes.push_back(store ? RowPlane{f, q, e, 0, 0} : RowPlane{q, f, e, 0, 0});
     }
-  const int chunk = chunk_rows_of((int64_t)n_kv_heads * head_dim * (int64_t)esz);
+  const int chunk = chunk_rows_of((int64_t)n_kv_heads * head_dim * (int64_t)esz, job.rows, 2 * (int64_t)n_layers);
   return move_rows(ctx, job.ranges, planes, chunk, s, [&](const RowsArgs &a, const RowsFew &few) {
     if (store && esz == 2) launch_rows_store<bf16>(a, few, n_kv_heads, head_dim, wide, s);
     else if (store) launch_rows_store<float>(a, few, n_kv_heads, head_dim, wide, s);
@@ -1714,6 +1717,10 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
     auto longer = [](const QAttnItem &x, const QAttnItem &y) { return x.kend - x.kbeg > y.kend - y.kbeg; };
     if (!std::is_sorted(c.items.begin(), c.items.end(), longer)) std::stable_sort(c.items.begin(), c.items.end(), longer);
   }
+  // (rows that all have every record need no counts)
+  bool all = true;
+  for (size_t i = 0; i < q.counts.size(); i += 2) all = all && q.counts[i] == n_own && q.counts[i + 1] == n_shared;
+  if (all) q.counts.clear();
   return q;
 }
 template <typename T>
@@ -1735,7 +1742,7 @@ void run_qattn(alora_ctx *ctx, const QAttnPlan &q, const char *staged, const Lay
       a.sm_scale = 1.0f / sqrtf((float)L.head_dim);
       a.partials = partials;
       a.out = direct ? out : nullptr;
-      if (!direct) mc = MergeCounts{(const int32_t *)(staged + q.item_bytes() + QAttnPlan::up(q.rows.size() * 4)), q.first_shared};
+      if (!q.counts.empty()) mc = MergeCounts{(const int32_t *)(staged + q.item_bytes() + QAttnPlan::up(q.rows.size() * 4)), q.first_shared};
       for (int k = 0; k < 2; ++k) {
         const QAttnClass &c = q.cls[k];
         const int n = (int)c.items.size();
@@ -1806,20 +1813,27 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   const QAttnPlan qp = plan_qattn(ctx, pl, L, qt, qattn_mfma_supported(ctx, L, *cache, q, out), qattn_lds_supported(L, *cache));
   st = ensure_workspace(ctx, qp.n_parts > 1 ? attn_plain_partial_floats(L, pl.T, qp.n_parts) * sizeof(float) : 0);
   if (st != ALORA_OK) return st;
-  const size_t seq_bytes = ((size_t)B * sizeof(SeqMeta) + 15) & ~(size_t)15;
+  const size_t seq_bytes = qp.mfma ? 0 : ((size_t)B * sizeof(SeqMeta) + 15) & ~(size_t)15;      // (the plain kernel reads the sequences' records)
   const size_t bytes = seq_bytes + qp.bytes();
   MetaSlot *slot = nullptr;
   st = acquire_slot(ctx, bytes, &slot);
   if (st != ALORA_OK) return st;
-  memcpy(slot->host, pl.seqs.data(), (size_t)B * sizeof(SeqMeta));
+  if (seq_bytes) memcpy(slot->host, pl.seqs.data(), (size_t)B * sizeof(SeqMeta));
   qp.write(slot->host + seq_bytes);
-  const int n16 = (int)(bytes / 16);
-  hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
-  const SeqMeta *seqs_dev = (const SeqMeta *)slot->dev;
+  // A workgroup reads one item: short lists stay where they are, in pinned host memory (five short sequences 18.6 -> 15.5 us, 64 long ones 204 -> 201;
+  // as much for lists of any length that was measured, 64 KB)
+  constexpr size_t QATTN_HOST_BYTES = 16384;
+  const char *at = slot->host;
+  if (!qp.mfma || bytes > QATTN_HOST_BYTES) {
+    const int n16 = (int)(bytes / 16);
+    hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
+    at = slot->dev;
+  }
+  const SeqMeta *seqs_dev = (const SeqMeta *)at;
   if (dtype == ALORA_BF16)
-    run_qattn<bf16>(ctx, qp, slot->dev + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, false, (bf16 *)out, s);
+    run_qattn<bf16>(ctx, qp, at + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, false, (bf16 *)out, s);
   else
-    run_qattn<float>(ctx, qp, slot->dev + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, false, (float *)out, s);
+    run_qattn<float>(ctx, qp, at + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, false, (float *)out, s);
   HIP_TRY(ctx, hipGetLastError());
   HIP_TRY(ctx, hipEventRecord(slot->ev, s));
   slot->in_flight = true;
@@ -2095,7 +2109,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   if (qc) {
     for (const SeqMeta &m : pl.seqs)
       if (m.n_new > 0) new_rows.push_back(RowRange{m.row_start, m.pool_off + m.P, m.n_new, 0});
-    store.chunk_rows = chunk_rows_of((int64_t)L.n_kv * (int64_t)esz);
+    store.chunk_rows = chunk_rows_of((int64_t)L.n_kv * (int64_t)esz, pl.T, 2);
     if (!cut_ranges(new_rows, store.chunk_rows, &store.n_chunks)) return fail(ctx, ALORA_EINVAL, "the call stores more rows than a grid takes");
     store.n_ranges = (int)new_rows.size();
     store.n_planes = 2;
@@ -2174,7 +2188,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     alora_kv_cache fresh{};
     fresh.k = ctx->ws + probe.bytes; fresh.v = ctx->ws + probe.bytes + new_bytes; fresh.pool_tokens = pl.T;
     project_rows<T>(ctx, &layers[l], L, &fresh, cur, ppl, seqs_dev, w, l == 0, 0, s);
-    const bool wide = L.head_dim % QBLOCK == 0 && ((uintptr_t)qc[l].k | (uintptr_t)qc[l].v) % 16 == 0;
+    const bool wide = L.head_dim % QBLOCK == 0 && ((uintptr_t)qc[l].k | (uintptr_t)qc[l].v) % 4 == 0;
     store.planes = (const RowPlane *)(slot->dev + q_at + qseq_bytes + qattn_bytes + range_bytes) + 2 * l;
     {
       ProfScope p(ctx, K_ROWS, s);

@@ -100,19 +100,135 @@ __global__ __launch_bounds__(256) void rows_load_any_kernel(RowsArgs a, RowsFew 
   }
 }
 
+// Whole blocks of 32 channels: four lanes share a block, a lane has 8 channels -- 16 bytes of bf16, 4 of codes -- so that both sides of a piece are one run of
+// memory.  WIDE_AHEAD such loads are on the way per lane.
+constexpr int WIDE_AHEAD = 4;
+typedef uint32_t rows_u32x4 __attribute__((ext_vector_type(4)));
+template <typename T> struct Wide8;
+template <> struct Wide8<bf16> {
+  rows_u32x4 w;
+  __device__ __forceinline__ void load(const bf16 *p) { w = __builtin_nontemporal_load(reinterpret_cast<const rows_u32x4 *>(p)); }
+  __device__ __forceinline__ float at(int i) const { return __builtin_bit_cast(float, i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max(m, max(w[i] & 0x7fff0000u, w[i] << 16 & 0x7fff0000u));
+    return m;
+  }
+};
+template <> struct Wide8<float> {
+  rows_u32x4 w[2];
+  __device__ __forceinline__ void load(const float *p) {
+    w[0] = __builtin_nontemporal_load(reinterpret_cast<const rows_u32x4 *>(p));
+    w[1] = __builtin_nontemporal_load(reinterpret_cast<const rows_u32x4 *>(p) + 1);
+  }
+  __device__ __forceinline__ float at(int i) const {
+    const uint32_t u = w[i >> 2][i & 3];      // (a bit cast of the element itself would take the vector's first)
+    return __builtin_bit_cast(float, u);
+  }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, w[i >> 2][i & 3] & 0x7fffffffu);
+    return m;
+  }
+};
+// the largest of a block's four lanes
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));      // lanes 1 0 3 2
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));   // lanes 2 3 0 1
+}
+
+template <typename T, bool FEW>
+__global__ __launch_bounds__(256) void rows_store_wide_kernel(RowsArgs a, RowsFew few, int row_pieces) {
+  const RowPlane pl = FEW ? few.planes[blockIdx.y] : a.planes[blockIdx.y];
+  const RowPiece p = row_piece(FEW ? few.ranges : a.ranges, a.n_ranges, blockIdx.x, a.chunk_rows);
+  const int n = p.rows * row_pieces;      // (a multiple of 4)
+  const T *src = (const T *)pl.src + p.src * row_pieces * 8;
+  uint32_t *dst = (uint32_t *)pl.dst + p.dst * row_pieces;
+  uint8_t *scale = (uint8_t *)pl.scale + p.dst * (row_pieces / 4);
+  for (int i0 = threadIdx.x; i0 < n; i0 += WIDE_AHEAD * 256) {
+    Wide8<T> x[WIDE_AHEAD];
+#pragma unroll
+    for (int u = 0; u < WIDE_AHEAD; ++u)
+      if (i0 + u * 256 < n) x[u].load(src + (int64_t)(i0 + u * 256) * 8);
+#pragma unroll
+    for (int u = 0; u < WIDE_AHEAD; ++u) {
+      const int i = i0 + u * 256;
+      if (i >= n) continue;
+      const int e = q_exponent(quad_max(x[u].top()));
+      const float sc = q_scale(e);
+      uint32_t w = 0;
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u].at(0), x[u].at(1), sc, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u].at(2), x[u].at(3), sc, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u].at(4), x[u].at(5), sc, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[u].at(6), x[u].at(7), sc, 3);
+      dst[i] = e == Q_E_NAN ? 0u : w;
+      if ((i & 3) == 0) scale[i >> 2] = (uint8_t)e;
+    }
+  }
+}
+
+template <typename T, bool FEW>
+__global__ __launch_bounds__(256) void rows_load_wide_kernel(RowsArgs a, RowsFew few, int row_pieces) {
+  const RowPlane pl = FEW ? few.planes[blockIdx.y] : a.planes[blockIdx.y];
+  const RowPiece p = row_piece(FEW ? few.ranges : a.ranges, a.n_ranges, blockIdx.x, a.chunk_rows);
+  const int n = p.rows * row_pieces;
+  const uint32_t *src = (const uint32_t *)pl.src + p.src * row_pieces;
+  const uint8_t *scale = (const uint8_t *)pl.scale + p.src * (row_pieces / 4);
+  T *dst = (T *)pl.dst + p.dst * row_pieces * 8;
+  for (int i0 = threadIdx.x; i0 < n; i0 += WIDE_AHEAD * 256) {
+    uint32_t w[WIDE_AHEAD], e[WIDE_AHEAD];
+#pragma unroll
+    for (int u = 0; u < WIDE_AHEAD; ++u)
+      if (i0 + u * 256 < n) { w[u] = src[i0 + u * 256]; e[u] = scale[(i0 + u * 256) >> 2]; }
+#pragma unroll
+    for (int u = 0; u < WIDE_AHEAD; ++u) {
+      const int i = i0 + u * 256;
+      if (i >= n) continue;
+      const float sc = q_scale((int)e[u]);      // (an exponent of 255 makes every code NaN)
+      if constexpr (sizeof(T) == 2) {
+        rows_u32x4 y;
+        y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[u], sc, 0));
+        y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[u], sc, 1));
+        y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[u], sc, 2));
+        y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[u], sc, 3));
+        __builtin_nontemporal_store(y, reinterpret_cast<rows_u32x4 *>(dst) + i);
+      } else {
+        rows_u32x4 y[2];
+        auto put = [&](int at, auto v) {
+          const float x0 = v[0], x1 = v[1];
+          y[at >> 2][at & 3] = __builtin_bit_cast(uint32_t, x0);
+          y[at >> 2][(at & 3) + 1] = __builtin_bit_cast(uint32_t, x1);
+        };
+        put(0, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], sc, 0));
+        put(2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], sc, 1));
+        put(4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], sc, 2));
+        put(6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], sc, 3));
+        __builtin_nontemporal_store(y[0], reinterpret_cast<rows_u32x4 *>(dst) + 2 * i);
+        __builtin_nontemporal_store(y[1], reinterpret_cast<rows_u32x4 *>(dst) + 2 * i + 1);
+      }
+    }
+  }
+}
+
 template <typename T> void launch_rows_store(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s) {
   if (a.n_chunks == 0 || a.n_planes == 0) return;
-  (void)wide;
   const dim3 grid((unsigned)a.n_chunks, (unsigned)a.n_planes);
-  auto kern = a.planes == nullptr ? rows_store_any_kernel<T, true> : rows_store_any_kernel<T, false>;
-  hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a, few, n_kv_heads, head_dim);
+  const bool f = a.planes == nullptr;
+  auto any = f ? rows_store_any_kernel<T, true> : rows_store_any_kernel<T, false>;
+  auto fast = f ? rows_store_wide_kernel<T, true> : rows_store_wide_kernel<T, false>;
+  if (wide) hipLaunchKernelGGL(fast, grid, dim3(256), 0, s, a, few, n_kv_heads * head_dim / 8);
+  else hipLaunchKernelGGL(any, grid, dim3(256), 0, s, a, few, n_kv_heads, head_dim);
 }
 template <typename T> void launch_rows_load(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s) {
   if (a.n_chunks == 0 || a.n_planes == 0) return;
-  (void)wide;
   const dim3 grid((unsigned)a.n_chunks, (unsigned)a.n_planes);
-  auto kern = a.planes == nullptr ? rows_load_any_kernel<T, true> : rows_load_any_kernel<T, false>;
-  hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a, few, n_kv_heads, head_dim);
+  const bool f = a.planes == nullptr;
+  auto any = f ? rows_load_any_kernel<T, true> : rows_load_any_kernel<T, false>;
+  auto fast = f ? rows_load_wide_kernel<T, true> : rows_load_wide_kernel<T, false>;
+  if (wide) hipLaunchKernelGGL(fast, grid, dim3(256), 0, s, a, few, n_kv_heads * head_dim / 8);
+  else hipLaunchKernelGGL(any, grid, dim3(256), 0, s, a, few, n_kv_heads, head_dim);
 }
 template void launch_rows_store<float>(const RowsArgs &, const RowsFew &, int, int, bool, hipStream_t);
 template void launch_rows_store<bf16>(const RowsArgs &, const RowsFew &, int, int, bool, hipStream_t);

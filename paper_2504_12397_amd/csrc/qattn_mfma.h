@@ -465,8 +465,8 @@ __device__ __forceinline__ void qa_dword_to_lds(i32x4 rsrc, int voff, int lds) {
   lds = __builtin_amdgcn_readfirstlane(lds);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
 }
-template <int HT, int NQ, int NP, int NC, int DEPTH, typename TQ, typename T>
-__global__ __launch_bounds__(512, 2) void qattn_lds_kernel(QAttnArgs a) {
+template <int HT, int NQ, int NP, int NC, int DEPTH, int OCC, typename TQ, typename T>
+__global__ __launch_bounds__(512, OCC) void qattn_lds_kernel(QAttnArgs a) {
   typedef QaTile<HT> Tile;
   typedef QaRing<HT, DEPTH> R;
   extern __shared__ __align__(16) char s_ring[];
@@ -527,6 +527,9 @@ __global__ __launch_bounds__(512, 2) void qattn_lds_kernel(QAttnArgs a) {
   int slot = 0;
   for (int k0 = w.kbeg; k0 < w.kend; k0 += 32) {
     wait_vm<(DEPTH - 1) * R::PER_STEP>();
+    // The heads of a token share lines of memory: waves that drift apart fetch them twice (64 x 16449 keys: 1.29 GB instead of 1.15, 248 us; so 206).
+    // (Waves of a workgroup have different numbers of steps where they share keys, and join through barriers there: not then.)
+    if (a.kr == 1) __builtin_amdgcn_s_barrier();
     const char *st = ring + slot * R::STAGE;
     Tile t;
 #pragma unroll
@@ -572,9 +575,9 @@ void qattn_mfma_start(const QAttnArgs &a, int n_items, hipStream_t s) {
   if (smem > 48 * 1024) (void)hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   hipLaunchKernelGGL(kern, dim3(n_items), dim3(64 * W), smem, s, a);
 }
-template <int HT, int NQ, int NP, int NC, int DEPTH, typename TQ, typename T>
+template <int HT, int NQ, int NP, int NC, int DEPTH, int OCC, typename TQ, typename T>
 void qattn_lds_start(const QAttnArgs &a, int n_items, hipStream_t s) {
-  auto kern = qattn_lds_kernel<HT, NQ, NP, NC, DEPTH, TQ, T>;
+  auto kern = qattn_lds_kernel<HT, NQ, NP, NC, DEPTH, OCC, TQ, T>;
   const size_t join = a.kr == 1 ? 0 : (size_t)4 * NC * (HT / 4 + 3) * 64 * sizeof(float), ring = (size_t)8 * QaRing<HT, DEPTH>::WAVE;
   const size_t smem = join > ring ? join : ring;
   static_assert(8 * QaRing<HT, DEPTH>::WAVE <= 160 * 1024 && 4 * NC * (HT / 4 + 3) * 256 <= 160 * 1024, "");

@@ -34,7 +34,7 @@ struct RowsArgs {
   int chunk_rows;
 };
 void launch_rows_copy(const RowsArgs &a, const RowsFew &few, hipStream_t s);
-// T rows of n_kv heads of head_dim <-> rows of 4 bits; wide: head_dim is a multiple of 32 and every base of 16 bytes (exponents: of 4)
+// T rows of n_kv heads of head_dim <-> rows of 4 bits; wide: head_dim is a multiple of 32, rows begin at multiples of 16 bytes, codes of 4
 template <typename T> void launch_rows_store(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);
 template <typename T> void launch_rows_load(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);
 
