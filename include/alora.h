@@ -345,15 +345,15 @@ typedef struct { int64_t src, dst, n; } alora_row_range;
  *   ranges    HOST [n_ranges]; rows outside a pool: ALORA_ECAPACITY; destination ranges that overlap each other, negative n: ALORA_EINVAL.
  *             n = 0 is allowed, and n_ranges = 0 is a valid no-op.
  * dst[l] and src[l] are the same arrays or do not overlap in memory (ALORA_EINVAL where bases differ and memory overlaps).  Rows that move
- * over others, in more than one order, are staged through the context's workspace. */
+ * over others, some towards the front and some towards the back, are staged through the context's workspace. */
 alora_status alora_cache_copy(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_kv_cache *dst,
                               const alora_kv_cache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
 /* The same for rows of 4 bits: codes and exponents. */
 alora_status alora_qcache_copy(alora_ctx *ctx, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *dst, const alora_qcache *src,
                                int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
-/* Rows of the storage type into rows of 4 bits, and back.  Ranges as above; dst and src never share memory.  All four calls with at most 16
- * ranges and 32 layers (copies of 4 bits: 16) launch one kernel and nothing else, unless rows move over each other: such a call may be captured into a HIP graph.
- * Under capture the others are refused (ALORA_EINVAL). */
+/* Rows of the storage type into rows of 4 bits, and back.  Ranges as above; dst and src never share memory.  Calls of all four kinds whose ranges and
+ * arrays travel as kernel arguments (24 bytes a range, 32 an array -- two a layer, four with 4 bits on both sides -- 3584 bytes in all) launch one kernel and
+ * nothing else, unless rows move over each other: such a call may be captured into a HIP graph.  Under capture the others are refused (ALORA_EINVAL). */
 alora_status alora_qcache_store(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *dst,
                                 const alora_kv_cache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
 alora_status alora_qcache_load(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_kv_cache *dst,

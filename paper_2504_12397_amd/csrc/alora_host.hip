@@ -100,6 +100,9 @@ struct alora_ctx {
   float2 *rope = nullptr;
   int rope_pos = 0, rope_half = 0;
   float rope_theta = 0.f;
+  uint32_t *flags = nullptr;     // ordered copies: ticket counters, then flags that hold the epoch of the call that set them
+  size_t flags_cap = 0;
+  uint32_t flags_epoch = 0;
   MetaSlot slots[N_SLOTS];
   int next_slot = 0;
   int opt_kernels = 0;
@@ -1393,7 +1396,8 @@ alora_status check_ranges(alora_ctx *ctx, const alora_row_range *r, int n, int64
       return fail(ctx, ALORA_ECAPACITY, "range %d: %lld destination rows from %lld on lie outside the pool of %lld tokens", i, (long long)r[i].n,
                   (long long)r[i].dst, (long long)dst_tokens);
     if (r[i].n == 0) continue;
-    const RowRange q{r[i].src, r[i].dst, r[i].n, 0};
+    if (r[i].n > 0x7fffffff) return fail(ctx, ALORA_EINVAL, "range %d: %lld rows are more than one range takes", i, (long long)r[i].n);
+    const RowRange q{r[i].src, r[i].dst, (uint32_t)r[i].n, 0};
     by_dst.push_back(q);
     if (in_place && q.src == q.dst) continue;
     job->ranges.push_back(q);
@@ -1420,15 +1424,12 @@ alora_status check_ranges(alora_ctx *ctx, const alora_row_range *r, int n, int64
 // Cuts the ranges in pieces of chunk_rows rows; false: too many for a grid.
 bool cut_ranges(std::vector<RowRange> &ranges, int chunk_rows, int64_t *n_chunks) {
   int64_t n = 0;
-  for (RowRange &q : ranges) { q.first_chunk = n; n += (q.n + chunk_rows - 1) / chunk_rows; }
+  for (RowRange &q : ranges) { q.first_chunk = (uint32_t)n; n += ((int64_t)q.n + chunk_rows - 1) / chunk_rows; }
   *n_chunks = n;
   return n <= 0x7fffffff;
 }
-// Rows of a piece: 4 to 32 KB of the widest array, 2048 workgroups where the call has that much
-int chunk_rows_of(int64_t row_bytes, int64_t rows, int64_t planes) {
-  const int64_t b = std::min<int64_t>(32768, std::max<int64_t>(4096, rows * planes * row_bytes / 2048));
-  return (int)std::max<int64_t>(1, std::min<int64_t>(4096, b / std::max<int64_t>(row_bytes, 1)));
-}
+// Rows of a piece: 32 KB of the widest array.  (Smaller pieces of small calls are slower: 17 rows of 2 KB in 64 arrays 16.8 us in pieces of 4 KB, 15.4 of 16 KB, 11.5 so.)
+int chunk_rows_of(int64_t row_bytes) { return (int)std::max<int64_t>(1, std::min<int64_t>(4096, 32768 / std::max<int64_t>(row_bytes, 1))); }
 
 // One launch over ranges x planes: `launch` gets the arguments.
 template <typename F>
@@ -1442,11 +1443,12 @@ alora_status move_rows(alora_ctx *ctx, std::vector<RowRange> ranges, const std::
   if (!cut_ranges(ranges, chunk_rows, &a.n_chunks) || a.n_planes > 65535) return fail(ctx, ALORA_EINVAL, "the call moves more rows than a grid takes");
   const bool cap = is_capturing(s);
   MetaSlot *slot = nullptr;
-  if (a.n_ranges <= ROW_FEW_RANGES && a.n_planes <= ROW_FEW_PLANES) {
-    memcpy(few.ranges, ranges.data(), ranges.size() * sizeof(RowRange));
-    memcpy(few.planes, planes.data(), planes.size() * sizeof(RowPlane));
+  if (rows_are_few(ranges.size(), planes.size())) {
+    a.planes_at = (int)rows_few_planes_at(ranges.size());
+    memcpy(few.data, ranges.data(), ranges.size() * sizeof(RowRange));
+    memcpy(few.data + a.planes_at, planes.data(), planes.size() * sizeof(RowPlane));
   } else {
-    if (cap) return fail(ctx, ALORA_EINVAL, "more than %d ranges or %d arrays: not under graph capture", ROW_FEW_RANGES, ROW_FEW_PLANES);
+    if (cap) return fail(ctx, ALORA_EINVAL, "%zu ranges of %zu arrays do not travel as kernel arguments: not under graph capture", ranges.size(), planes.size());
     const size_t rb = (ranges.size() * sizeof(RowRange) + 15) & ~(size_t)15, pb = (planes.size() * sizeof(RowPlane) + 15) & ~(size_t)15;
     alora_status st = acquire_slot(ctx, rb + pb, &slot);
     if (st != ALORA_OK) return st;
@@ -1471,13 +1473,94 @@ alora_status move_rows(alora_ctx *ctx, std::vector<RowRange> ranges, const std::
   return ALORA_OK;
 }
 
-int copy_unit(const void *dst, const void *src, int64_t row_bytes) {
+uint32_t copy_unit(const void *dst, const void *src, int64_t row_bytes) {
   const uintptr_t m = (uintptr_t)dst | (uintptr_t)src | (uintptr_t)row_bytes;
   return m % 16 == 0 ? 16 : m % 4 == 0 ? 4 : 1;
 }
 
 // An array of one layer as alora_cache_copy and alora_qcache_copy see it.
 struct CopyArray { const void *src; void *dst; int64_t row_bytes; };
+
+// Rows of one pool that move over each other, all in one direction, in one pass (RowsOrderedArgs).  *done: they have been; otherwise the ranges or the
+// rows do not suit it.
+alora_status copy_rows_ordered(alora_ctx *ctx, const RowJob &job, const std::vector<CopyArray> &arrays, hipStream_t s, bool *done) {
+  *done = false;
+  const bool down = job.ranges[0].src > job.ranges[0].dst;
+  for (const RowRange &q : job.ranges)
+    if ((q.src > q.dst) != down) return ALORA_OK;
+  std::vector<RowPlane> planes;
+  int64_t chunk = 4096, widest = 0;
+  for (const CopyArray &c : arrays) {
+    const uint32_t unit = copy_unit(c.dst, c.src, c.row_bytes);
+    chunk = std::min(chunk, (int64_t)ROWS_ORDERED_UNITS * unit / c.row_bytes);
+    widest = std::max(widest, c.row_bytes);
+    planes.push_back(RowPlane{c.src, c.dst, nullptr, (uint32_t)c.row_bytes, unit});
+  }
+  if (chunk < 1 || planes.size() > ROWS_ORDERED_PLANES) return ALORA_OK;
+  chunk = std::min<int64_t>(chunk, chunk_rows_of(widest));
+  std::vector<RowRange> r(job.ranges);
+  std::sort(r.begin(), r.end(), [&](const RowRange &x, const RowRange &y) { return down ? x.dst < y.dst : x.dst > y.dst; });
+  std::vector<RowStep> steps;
+  for (const RowRange &q : r)
+    for (int64_t at = 0; at < q.n; at += chunk) {
+      const int64_t n = std::min<int64_t>(chunk, q.n - at), off = down ? at : q.n - at - n;
+      steps.push_back(RowStep{q.src + off, q.dst + off, (int32_t)n, 0, 0, 0});
+    }
+  if ((int64_t)steps.size() * (int64_t)planes.size() > (1 << 24)) return ALORA_OK;
+  // the pieces whose sources a destination covers: by their sources' order, the smallest and the largest place of them
+  std::vector<int> by_src(steps.size());
+  for (size_t i = 0; i < steps.size(); ++i) by_src[i] = (int)i;
+  std::sort(by_src.begin(), by_src.end(), [&](int x, int y) { return steps[x].src < steps[y].src; });
+  // (sources may overlap each other: a piece that begins before this destination ends at most `chunk` rows further on)
+  for (size_t i = 0; i < steps.size(); ++i) {
+    RowStep &st = steps[i];
+    auto lo = std::lower_bound(by_src.begin(), by_src.end(), st.dst - chunk, [&](int x, int64_t v) { return steps[x].src < v; });
+    int first = (int)steps.size(), last = -1;
+    for (; lo != by_src.end() && steps[*lo].src < st.dst + st.rows; ++lo)
+      if (steps[*lo].src + steps[*lo].rows > st.dst) { first = std::min(first, *lo); last = std::max(last, *lo); }
+    if (last >= 0) { st.dep0 = first; st.dep1 = std::min(last, (int)i) + 1; }      // (none comes after it)
+  }
+  const size_t tickets = (size_t)ROWS_ORDERED_PLANES * ROWS_TICKET_STRIDE, want = tickets + steps.size() * planes.size();
+  if (ctx->flags_cap < want) {
+    HIP_TRY(ctx, hipDeviceSynchronize());
+    if (ctx->flags) HIP_TRY(ctx, hipFree(ctx->flags));
+    ctx->flags = nullptr;
+    ctx->flags_cap = 0;
+    const size_t cap = std::max<size_t>(4096, want + want / 2);
+    HIP_TRY(ctx, hipMalloc((void **)&ctx->flags, cap * sizeof(uint32_t)));
+    HIP_TRY(ctx, hipMemset(ctx->flags, 0, cap * sizeof(uint32_t)));
+    ctx->flags_cap = cap;
+    ctx->flags_epoch = 0;
+    HIP_TRY(ctx, hipDeviceSynchronize());
+  }
+  if (++ctx->flags_epoch == 0) {      // (every 2^32 calls the flags begin anew)
+    HIP_TRY(ctx, hipDeviceSynchronize());
+    HIP_TRY(ctx, hipMemset(ctx->flags, 0, ctx->flags_cap * sizeof(uint32_t)));
+    HIP_TRY(ctx, hipDeviceSynchronize());
+    ctx->flags_epoch = 1;
+  }
+  const size_t sb = steps.size() * sizeof(RowStep), pb = (planes.size() * sizeof(RowPlane) + 15) & ~(size_t)15;
+  MetaSlot *slot = nullptr;
+  const alora_status got = acquire_slot(ctx, sb + pb, &slot);
+  if (got != ALORA_OK) return got;
+  memcpy(slot->host, steps.data(), sb);
+  memcpy(slot->host + sb, planes.data(), planes.size() * sizeof(RowPlane));
+  const char *at = slot->host;      // short lists are read where they are
+  if (sb + pb > 16384) {
+    const int n16 = (int)((sb + pb) / 16);
+    hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
+    at = slot->dev;
+  }
+  {
+    ProfScope p(ctx, K_ROWS, s);
+    launch_rows_copy_ordered(RowsOrderedArgs{(const RowStep *)at, (const RowPlane *)(at + sb), (int)steps.size(), (int)planes.size(), ctx->flags, ctx->flags + tickets, ctx->flags_epoch}, s);
+  }
+  HIP_TRY(ctx, hipGetLastError());
+  HIP_TRY(ctx, hipEventRecord(slot->ev, s));
+  slot->in_flight = true;
+  *done = true;
+  return ALORA_OK;
+}
 
 alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int64_t src_tokens, int64_t dst_tokens, const alora_row_range *ranges,
                        int n_ranges, hipStream_t s) {
@@ -1498,18 +1581,21 @@ alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int
   if (job.ranges.empty()) return ALORA_OK;
   if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
   HIP_TRY(ctx, hipSetDevice(ctx->device));
-  const int chunk = chunk_rows_of(widest, job.rows, (int64_t)arrays.size());
+  const int chunk = chunk_rows_of(widest);
   auto copy = [&](const std::vector<RowRange> &r, const std::vector<RowPlane> &planes) {
     return move_rows(ctx, r, planes, chunk, s, [&](const RowsArgs &a, const RowsFew &few) { launch_rows_copy(a, few, s); });
   };
   std::vector<RowPlane> planes;
+  bool done = false;
   if (!job.over) {
-    for (const CopyArray &c : arrays) planes.push_back(RowPlane{c.src, c.dst, nullptr, c.row_bytes, copy_unit(c.dst, c.src, c.row_bytes)});
+    for (const CopyArray &c : arrays) planes.push_back(RowPlane{c.src, c.dst, nullptr, (uint32_t)c.row_bytes, copy_unit(c.dst, c.src, c.row_bytes)});
     return copy(job.ranges, planes);
   }
-  // Rows that move over each other: through the workspace, as many arrays at a time as keep it at 128 MB (half of what the last-level cache holds),
-  // one at least.
   if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "rows that move over each other: not under graph capture");
+  st = copy_rows_ordered(ctx, job, arrays, s, &done);
+  if (st != ALORA_OK || done) return st;
+  // The others: through the workspace, as many arrays at a time as keep it at 128 MB (half of what the last-level cache holds),
+  // one at least.
   std::vector<RowRange> out(job.ranges), back(job.ranges);
   int64_t at = 0;
   for (size_t i = 0; i < out.size(); ++i) { out[i].dst = at; back[i].src = at; at += out[i].n; }
@@ -1527,9 +1613,9 @@ alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int
     for (; i < j; ++i) {
       const CopyArray &c = arrays[i];
       char *tmp = w.take<char>((size_t)job.rows * c.row_bytes);
-      const int unit = copy_unit(c.dst, c.src, c.row_bytes);
-      to.push_back(RowPlane{c.src, tmp, nullptr, c.row_bytes, unit});
-      from.push_back(RowPlane{tmp, c.dst, nullptr, c.row_bytes, unit});
+      const uint32_t unit = copy_unit(c.dst, c.src, c.row_bytes), row_bytes = (uint32_t)c.row_bytes;
+      to.push_back(RowPlane{c.src, tmp, nullptr, row_bytes, unit});
+      from.push_back(RowPlane{tmp, c.dst, nullptr, row_bytes, unit});
     }
     st = copy(out, to);
     if (st == ALORA_OK) st = copy(back, from);
@@ -1582,7 +1668,7 @@ alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_di
       wide = wide && (uintptr_t)f % 16 == 0 && (uintptr_t)q % 4 == 0;
       planes.push_back(store ? RowPlane{f, q, e, 0, 0} : RowPlane{q, f, e, 0, 0});
     }
-  const int chunk = chunk_rows_of((int64_t)n_kv_heads * head_dim * (int64_t)esz, job.rows, 2 * (int64_t)n_layers);
+  const int chunk = chunk_rows_of((int64_t)n_kv_heads * head_dim * (int64_t)esz);
   return move_rows(ctx, job.ranges, planes, chunk, s, [&](const RowsArgs &a, const RowsFew &few) {
     if (store && esz == 2) launch_rows_store<bf16>(a, few, n_kv_heads, head_dim, wide, s);
     else if (store) launch_rows_store<float>(a, few, n_kv_heads, head_dim, wide, s);
@@ -2108,8 +2194,8 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   RowsArgs store{};
   if (qc) {
     for (const SeqMeta &m : pl.seqs)
-      if (m.n_new > 0) new_rows.push_back(RowRange{m.row_start, m.pool_off + m.P, m.n_new, 0});
-    store.chunk_rows = chunk_rows_of((int64_t)L.n_kv * (int64_t)esz, pl.T, 2);
+      if (m.n_new > 0) new_rows.push_back(RowRange{m.row_start, m.pool_off + m.P, (uint32_t)m.n_new, 0});
+    store.chunk_rows = chunk_rows_of((int64_t)L.n_kv * (int64_t)esz);
     if (!cut_ranges(new_rows, store.chunk_rows, &store.n_chunks)) return fail(ctx, ALORA_EINVAL, "the call stores more rows than a grid takes");
     store.n_ranges = (int)new_rows.size();
     store.n_planes = 2;
@@ -2289,6 +2375,7 @@ void alora_destroy(alora_ctx *ctx) {
   (void)hipDeviceSynchronize();
   if (ctx->ws) (void)hipFree(ctx->ws);
   if (ctx->rope) (void)hipFree(ctx->rope);
+  if (ctx->flags) (void)hipFree(ctx->flags);
   (void)drain_profile(ctx);
   for (hipEvent_t e : ctx->prof_free) (void)hipEventDestroy(e);
   for (MetaSlot &sl : ctx->slots) {

@@ -4,24 +4,31 @@
 
 namespace alora {
 
-// The piece of a range that workgroup x of the launch moves: binary search over the ranges' first pieces (uniform, scalar loads).
+// The piece of a range that workgroup x of the launch moves (binary search over the ranges' first pieces, uniform, unless every range is one), and the
+// array that workgroup y does.
 struct RowPiece { int64_t src, dst; int rows; };
-__device__ __forceinline__ RowPiece row_piece(const RowRange *ranges, int n_ranges, int64_t chunk, int chunk_rows) {
-  int lo = 0, hi = n_ranges - 1;
+template <bool FEW> __device__ __forceinline__ RowPiece row_piece(const RowsArgs &a, const RowsFew &few) {
+  const RowRange *ranges = FEW ? reinterpret_cast<const RowRange *>(few.data) : a.ranges;
+  const uint32_t chunk = blockIdx.x;
+  int lo = 0, hi = a.n_ranges - 1;
+  if (a.n_chunks == a.n_ranges) lo = hi = (int)chunk;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (ranges[mid].first_chunk <= chunk) lo = mid; else hi = mid - 1;
   }
   const RowRange r = ranges[lo];
-  const int64_t at = (chunk - r.first_chunk) * chunk_rows, left = r.n - at;
-  return RowPiece{r.src + at, r.dst + at, (int)(left < chunk_rows ? left : chunk_rows)};
+  const int64_t at = (int64_t)(chunk - r.first_chunk) * a.chunk_rows, left = r.n - at;
+  return RowPiece{r.src + at, r.dst + at, (int)(left < a.chunk_rows ? left : a.chunk_rows)};
+}
+template <bool FEW> __device__ __forceinline__ RowPlane row_plane(const RowsArgs &a, const RowsFew &few) {
+  return FEW ? reinterpret_cast<const RowPlane *>(few.data + a.planes_at)[blockIdx.y] : a.planes[blockIdx.y];
 }
 
 template <typename U>
 __device__ __forceinline__ void copy_piece(const RowPlane &pl, const RowPiece &p) {
   const U *src = reinterpret_cast<const U *>((const char *)pl.src + p.src * pl.row_bytes);
   U *dst = reinterpret_cast<U *>((char *)pl.dst + p.dst * pl.row_bytes);
-  const int64_t n = p.rows * pl.row_bytes / (int64_t)sizeof(U);
+  const int64_t n = p.rows * (int64_t)pl.row_bytes / (int64_t)sizeof(U);
   for (int64_t i0 = threadIdx.x; i0 < n; i0 += 4 * 256) {      // four pieces on the way
     U v[4];
 #pragma unroll
@@ -35,8 +42,8 @@ __device__ __forceinline__ void copy_piece(const RowPlane &pl, const RowPiece &p
 
 template <bool FEW>
 __global__ __launch_bounds__(256) void rows_copy_kernel(RowsArgs a, RowsFew few) {
-  const RowPlane pl = FEW ? few.planes[blockIdx.y] : a.planes[blockIdx.y];
-  const RowPiece p = row_piece(FEW ? few.ranges : a.ranges, a.n_ranges, blockIdx.x, a.chunk_rows);
+  const RowPlane pl = row_plane<FEW>(a, few);
+  const RowPiece p = row_piece<FEW>(a, few);
   if (pl.unit == 16) copy_piece<uint4>(pl, p);
   else if (pl.unit == 4) copy_piece<uint32_t>(pl, p);
   else copy_piece<uint8_t>(pl, p);
@@ -47,6 +54,51 @@ void launch_rows_copy(const RowsArgs &a, const RowsFew &few, hipStream_t s) {
   const dim3 grid((unsigned)a.n_chunks, (unsigned)a.n_planes);
   auto kern = a.planes == nullptr ? rows_copy_kernel<true> : rows_copy_kernel<false>;
   hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a, few);
+}
+
+// Workgroups take the pieces of their array by tickets, so that one only ever waits for pieces that running workgroups have taken, and those for earlier ones: every
+// wait ends.  One pass over memory, where staging takes two (a workspace written and read).
+// (U: what is moved at a time; R: the register it waits in)
+template <typename U, typename R>
+__device__ __forceinline__ void ordered_piece(const RowsOrderedArgs &a, const RowPlane &pl, const RowStep &st, int step, int plane) {
+  const U *src = reinterpret_cast<const U *>((const char *)pl.src + st.src * pl.row_bytes);
+  U *dst = reinterpret_cast<U *>((char *)pl.dst + st.dst * pl.row_bytes);
+  const int n = (int)((int64_t)st.rows * pl.row_bytes / (int)sizeof(U)), tid = threadIdx.x;      // <= ROWS_ORDERED_UNITS
+  R v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = tid + j * 256 < n ? (R)src[tid + j * 256] : R{};
+  // The piece is in registers before anyone is told so.  (No data passes between workgroups, only that: relaxed flags; acquiring and releasing would write the
+  // caches back and empty them at every piece: 75000 rows of 1088 bytes in four layers 1470 us, so 205; through a workspace 385.)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) __hip_atomic_store(a.read + (int64_t)step * a.n_planes + plane, a.epoch, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int d = st.dep0 + tid; d < st.dep1; d += 256)
+    if (d != step)
+      while (__hip_atomic_load(a.read + (int64_t)d * a.n_planes + plane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.epoch) __builtin_amdgcn_s_sleep(1);
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (tid + j * 256 < n) dst[tid + j * 256] = (U)v[j];
+}
+__global__ __launch_bounds__(256) void rows_copy_ordered_kernel(RowsOrderedArgs a) {
+  __shared__ uint32_t s_step;
+  const int plane = (int)(blockIdx.x % (uint32_t)a.n_planes);
+  if (threadIdx.x == 0) {
+    uint32_t *ticket = a.ticket + plane * ROWS_TICKET_STRIDE;
+    s_step = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (s_step == (uint32_t)a.n_steps - 1) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // (the last one: nobody else takes any)
+  }
+  __syncthreads();
+  const int step = __builtin_amdgcn_readfirstlane((int)s_step);
+  if (step >= a.n_steps) return;
+  const RowPlane pl = a.planes[plane];
+  const RowStep st = a.steps[step];
+  if (pl.unit == 16) ordered_piece<uint4, uint4>(a, pl, st, step, plane);
+  else if (pl.unit == 4) ordered_piece<uint32_t, uint32_t>(a, pl, st, step, plane);
+  else ordered_piece<uint8_t, uint32_t>(a, pl, st, step, plane);
+}
+void launch_rows_copy_ordered(const RowsOrderedArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL(rows_copy_ordered_kernel, dim3((unsigned)a.n_steps * (unsigned)a.n_planes), dim3(256), 0, s, a);
 }
 
 // ---- rows of the storage type <-> rows of 4 bits -------------------------------------------------------------
@@ -63,8 +115,8 @@ __device__ __forceinline__ uint32_t abs_bits(float v) { return __builtin_bit_cas
 // One thread per block of 32 channels, any head size and alignment.
 template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void rows_store_any_kernel(RowsArgs a, RowsFew few, int n_kv_heads, int head_dim) {
-  const RowPlane pl = FEW ? few.planes[blockIdx.y] : a.planes[blockIdx.y];
-  const RowPiece p = row_piece(FEW ? few.ranges : a.ranges, a.n_ranges, blockIdx.x, a.chunk_rows);
+  const RowPlane pl = row_plane<FEW>(a, few);
+  const RowPiece p = row_piece<FEW>(a, few);
   const int nb = q_blocks(head_dim), per_row = n_kv_heads * nb;
   for (int i = threadIdx.x; i < p.rows * per_row; i += 256) {
     const int r = i / per_row, hb = i - r * per_row, g = hb / nb, blk = hb - g * nb;
@@ -85,8 +137,8 @@ __global__ __launch_bounds__(256) void rows_store_any_kernel(RowsArgs a, RowsFew
 template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void rows_load_any_kernel(RowsArgs a, RowsFew few, int n_kv_heads, int head_dim) {
   typedef float f32x2_t __attribute__((ext_vector_type(2)));
-  const RowPlane pl = FEW ? few.planes[blockIdx.y] : a.planes[blockIdx.y];
-  const RowPiece p = row_piece(FEW ? few.ranges : a.ranges, a.n_ranges, blockIdx.x, a.chunk_rows);
+  const RowPlane pl = row_plane<FEW>(a, few);
+  const RowPiece p = row_piece<FEW>(a, few);
   const int nb = q_blocks(head_dim), half = head_dim / 2, per_row = n_kv_heads * half;
   for (int i = threadIdx.x; i < p.rows * per_row; i += 256) {
     const int r = i / per_row, hb = i - r * per_row, g = hb / half, c2 = hb - g * half;
@@ -141,8 +193,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 
 template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void rows_store_wide_kernel(RowsArgs a, RowsFew few, int row_pieces) {
-  const RowPlane pl = FEW ? few.planes[blockIdx.y] : a.planes[blockIdx.y];
-  const RowPiece p = row_piece(FEW ? few.ranges : a.ranges, a.n_ranges, blockIdx.x, a.chunk_rows);
+  const RowPlane pl = row_plane<FEW>(a, few);
+  const RowPiece p = row_piece<FEW>(a, few);
   const int n = p.rows * row_pieces;      // (a multiple of 4)
   const T *src = (const T *)pl.src + p.src * row_pieces * 8;
   uint32_t *dst = (uint32_t *)pl.dst + p.dst * row_pieces;
@@ -171,8 +223,8 @@ __global__ __launch_bounds__(256) void rows_store_wide_kernel(RowsArgs a, RowsFe
 
 template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void rows_load_wide_kernel(RowsArgs a, RowsFew few, int row_pieces) {
-  const RowPlane pl = FEW ? few.planes[blockIdx.y] : a.planes[blockIdx.y];
-  const RowPiece p = row_piece(FEW ? few.ranges : a.ranges, a.n_ranges, blockIdx.x, a.chunk_rows);
+  const RowPlane pl = row_plane<FEW>(a, few);
+  const RowPiece p = row_piece<FEW>(a, few);
   const int n = p.rows * row_pieces;
   const uint32_t *src = (const uint32_t *)pl.src + p.src * row_pieces;
   const uint8_t *scale = (const uint8_t *)pl.scale + p.src * (row_pieces / 4);

@@ -18,22 +18,41 @@ struct RowPlane {
   const void *src;
   void *dst;
   void *scale;             // store: written; load: read
-  int64_t row_bytes;       // copy ...
-  int64_t unit;            // ... in pieces of 16, 4 or 1 bytes, which both bases and the rows are multiples of
+  uint32_t row_bytes;      // copy ...
+  uint32_t unit;           // ... in pieces of 16, 4 or 1 bytes, which both bases and the rows are multiples of
 };
 // n rows from src on go to dst on; first_chunk: how many pieces of chunk_rows rows the ranges before it are cut in
-struct RowRange { int64_t src, dst, n, first_chunk; };
-// Few planes and ranges travel as kernel arguments (no staging kernel before the copy, and a captured call keeps them); more of them in device memory.
-constexpr int ROW_FEW_RANGES = 16, ROW_FEW_PLANES = 64;
-struct RowsFew { RowRange ranges[ROW_FEW_RANGES]; RowPlane planes[ROW_FEW_PLANES]; };
+struct RowRange { int64_t src, dst; uint32_t n, first_chunk; };
+// Few of both travel as kernel arguments (no staging kernel before the copy, and a captured call keeps them): ranges, then planes.  More of them
+// lie in device memory.
+constexpr int ROWS_FEW_BYTES = 3584;
+struct RowsFew { alignas(16) char data[ROWS_FEW_BYTES]; };
+inline size_t rows_few_planes_at(size_t n_ranges) { return (n_ranges * sizeof(RowRange) + 15) & ~(size_t)15; }
+inline bool rows_are_few(size_t n_ranges, size_t n_planes) { return rows_few_planes_at(n_ranges) + n_planes * sizeof(RowPlane) <= ROWS_FEW_BYTES; }
 struct RowsArgs {
   const RowRange *ranges;        // both nullptr: in `few`
   const RowPlane *planes;
   int n_ranges, n_planes;
   int64_t n_chunks;              // of all ranges
   int chunk_rows;
+  int planes_at;                 // in `few`
 };
 void launch_rows_copy(const RowsArgs &a, const RowsFew &few, hipStream_t s);
+// Rows that move over each other, all of them towards the front (or all towards the back) of one pool: pieces in the order of their destinations, from
+// the end that they move to.  A piece is read, says so, and is written once the pieces dep0 .. dep1 - 1 -- those whose sources its destination
+// covers, all of them before it -- have been read.
+struct RowStep { int64_t src, dst; int32_t rows, dep0, dep1, pad_; };
+struct RowsOrderedArgs {
+  const RowStep *steps;
+  const RowPlane *planes;
+  int n_steps, n_planes;
+  uint32_t *ticket;              // [n_planes], ROWS_TICKET_STRIDE apart (a line of memory each: one counter for all was 290 us of 19000 workgroups); 0 before and after a call
+  uint32_t *read;                // [n_steps, n_planes]: `epoch` once the piece has been read
+  uint32_t epoch;                // another one for every call on these flags
+};
+constexpr int ROWS_TICKET_STRIDE = 32, ROWS_ORDERED_PLANES = 1024;
+constexpr int ROWS_ORDERED_UNITS = 256 * 8;      // most units that a piece of any plane has
+void launch_rows_copy_ordered(const RowsOrderedArgs &a, hipStream_t s);
 // T rows of n_kv heads of head_dim <-> rows of 4 bits; wide: head_dim is a multiple of 32, rows begin at multiples of 16 bytes, codes of 4
 template <typename T> void launch_rows_store(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);
 template <typename T> void launch_rows_load(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);

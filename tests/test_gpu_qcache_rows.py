@@ -61,6 +61,8 @@ FORKS = [(10, 300, 50), (10, 350, 50), (12, 400, 3)]
 MANY = [(2 * i, 350 + 3 * i, 1 + i % 2) for i in range(80)]
 DOWN = [(5, 0, 100), (110, 100, 200), (330, 300, 1), (340, 301, 250)]                # over each other, towards the front
 UP = [(0, 7, 100), (100, 130, 200), (301, 349, 350)]                                  # towards the back
+CLOSE = [(4 + 23 * i, 2 + 20 * i, 20) for i in range(30)]                             # a pool that is closed up: a little more at every sequence
+SHUFFLED = [(400, 0, 120), (150, 120, 60), (600, 180, 90), (300, 270, 25), (299, 296, 3)]
 SWAP = [(0, 300, 200), (300, 0, 200), (250, 250, 20)]
 ROTATE = [(0, 100, 100), (100, 200, 100), (200, 0, 100), (500, 501, 150)]
 ONE_OVER_ITSELF = [(100, 101, 599)]
@@ -68,8 +70,8 @@ BACK_BY_ONE = [(1, 0, 699)]
 
 
 @pytest.mark.parametrize("same", [False, True], ids=["other_pool", "in_place"])
-@pytest.mark.parametrize("ranges", [DISJOINT, FORKS, MANY, DOWN, UP, SWAP, ROTATE, ONE_OVER_ITSELF, BACK_BY_ONE, []],
-                         ids=["disjoint", "forks", "many", "down", "up", "swap", "rotate", "over_itself", "back_by_one", "none"])
+@pytest.mark.parametrize("ranges", [DISJOINT, FORKS, MANY, DOWN, UP, CLOSE, SHUFFLED, SWAP, ROTATE, ONE_OVER_ITSELF, BACK_BY_ONE, []],
+                         ids=["disjoint", "forks", "many", "down", "up", "close", "shuffled", "swap", "rotate", "over_itself", "back_by_one", "none"])
 @pytest.mark.parametrize("kind,layers,heads,h", [("bf16", 3, 8, 128), ("f32", 1, 5, 80), ("bf16", 40, 1, 2), ("bf16", 2, 3, 6),
                                                  ("four", 3, 8, 128), ("four", 17, 3, 34), ("four", 1, 1, 2)])
 def test_copy(ab, ctx, kind, layers, heads, h, ranges, same):
@@ -86,6 +88,19 @@ def test_copy(ab, ctx, kind, layers, heads, h, ranges, same):
         if not same:
             for got, w in zip(arrays(src[l]), kept[l]):
                 assert torch.equal(bits(got), w), f"source of layer {l} changed"
+
+
+def test_long_moves_over_each_other_again_and_again(ab, ctx):
+    """Thousands of pieces in both directions, one call after the other on the same flags."""
+    rows = 60000
+    c = full_caches(ab, 2, rows, 8, 128, "bf16", 31)
+    want = [[bits(t).clone() for t in (x.k, x.v)] for x in c]
+    for ranges in ([(3, 0, 59997)], [(0, 1, 30000), (30002, 30050, 29000)], [(7 + 607 * i, 600 * i, 600) for i in range(90)],
+                   [(0, 700, 59000)], [(1, 0, 59999)]):
+        ab.alora_cache_copy(ctx, c, c, ranges)
+        want = [[moved(t, t, ranges) for t in x] for x in want]
+        for x, w in zip(c, want):
+            assert torch.equal(bits(x.k), w[0]) and torch.equal(bits(x.v), w[1])
 
 
 def awkward(rows, heads, h, dtype, seed):
@@ -178,14 +193,15 @@ def test_another_stream_and_a_captured_call(ab, ctx):
     def want():
         return torch.from_numpy(qref.values(*qref.quantise(src[1].k[3:23].cpu().double().numpy()))).to(torch.bfloat16)
     assert torch.equal(dst[1].k[:20].cpu(), want())
+    many = full_caches(ab, 1, 800, 2, 8, "bf16", 10)
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         ab.alora_cache_copy(ctx, src, src, [(40, 3, 20)])
         ab.alora_qcache_store(ctx, four, src, ranges)
         ab.alora_qcache_load(ctx, dst, four, [(10, 0, 20)])
-        for over in ([(0, 1, 20)], [(i, 30 + i, 1) for i in range(17)]):       # staged: refused, and the capture goes on
+        for c, over in ((src, [(0, 1, 20)]), (many, [(i, 400 + 2 * i, 1) for i in range(160)])):       # staged: refused, and the capture goes on
             with pytest.raises(ab.AloraError) as e:
-                ab.alora_cache_copy(ctx, src, src, over)
+                ab.alora_cache_copy(ctx, c, c, over)
             assert e.value.status == ab.ALORA_EINVAL
     for n in range(3):
         src[1].k[40:60] = torch.randn((20, 8, 128), generator=torch.Generator().manual_seed(n)).to(torch.bfloat16).cuda()
