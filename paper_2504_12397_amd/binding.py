@@ -95,12 +95,14 @@ def load_library() -> C.CDLL:
     lib.alora_stack_decode.restype = C.c_int
     lib.alora_stack_decode.argtypes = [C.c_void_p, C.POINTER(LayerDesc), C.c_int32, C.POINTER(KVCacheDesc), C.c_void_p,
                                        C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32, C.c_void_p, C.c_void_p]
-    i32, kvp, qp, rp, vp = C.c_int32, C.POINTER(KVCacheDesc), C.POINTER(QCacheDesc), C.POINTER(RowRange), C.c_void_p
+    # (arrays of descriptors, ranges and lengths go as addresses: the calls are short, and ctypes' typed pointers are not)
+    i32, vp = C.c_int32, C.c_void_p
+    kvp = qp = rp = vp
     lib.alora_cache_copy.argtypes = [vp, i32, i32, i32, kvp, kvp, i32, rp, i32, vp]
     lib.alora_qcache_copy.argtypes = [vp, i32, i32, qp, qp, i32, rp, i32, vp]
     lib.alora_qcache_store.argtypes = [vp, i32, i32, i32, qp, kvp, i32, rp, i32, vp]
     lib.alora_qcache_load.argtypes = [vp, i32, i32, i32, kvp, qp, i32, rp, i32, vp]
-    lib.alora_qcache_attend.argtypes = [vp, i32, i32, i32, i32, qp, vp, i32p, i32, vp, vp]
+    lib.alora_qcache_attend.argtypes = [vp, i32, i32, i32, i32, qp, vp, vp, i32, vp, vp]
     lib.alora_qcache_prefill.argtypes = [vp, C.POINTER(LayerDesc), qp, vp, i32p, i32p, i32p, i32, vp, vp]
     lib.alora_qcache_decode.argtypes = [vp, C.POINTER(LayerDesc), qp, vp, i32p, i32p, i32, vp, vp]
     lib.alora_qcache_stack_prefill.argtypes = [vp, C.POINTER(LayerDesc), i32, qp, vp, i32p, i32p, i32p, i32, vp, vp]
@@ -229,6 +231,10 @@ class KVCache(_Pool):
         self = cls.__new__(cls)
         self.k, self.v = k, v
         return self._wrap(k.shape[0], seq_offset, seq_capacity, seq_len, prefix_offset, prefix_len)
+
+    @property
+    def head_dim(self) -> int:
+        return int(self.k.shape[2])
 
     def _refresh(self):
         self.desc = KVCacheDesc(_ptr(self.k), _ptr(self.v), self.pool_tokens, *self._tables())
@@ -433,90 +439,58 @@ def alora_stack_decode(ctx: Context, layers: List[Layer], caches: List[KVCache],
 
 
 # ---- rows of a cache: copying them, and holding them in 4 bits ---------------------------------------------------
-def _ranges(ranges) -> np.ndarray:
+_DTYPES = {torch.float32: ALORA_F32, torch.bfloat16: ALORA_BF16}
+
+
+def _address(a: np.ndarray) -> int:
+    return a.__array_interface__["data"][0]
+
+
+def _move(name: str, ctx: Context, dst, src, ranges, stream, typed=None):
+    """The four calls that move rows: caches are one, or a list of them, one per layer; typed: the side whose type the call is told."""
+    d, s = ([dst] if isinstance(dst, _Pool) else dst), ([src] if isinstance(src, _Pool) else src)
+    if len(d) != len(s):
+        raise ValueError(f"{len(d)} destination and {len(s)} source layers")
+    shapes = [(int(c.k.shape[1]), c.head_dim) for c in (d[0], s[0])]
+    if shapes[0] != shapes[1] or (typed is None and d[0].k.dtype != s[0].k.dtype):
+        raise ValueError(f"caches of different shapes or types: {shapes[0]} {d[0].k.dtype} and {shapes[1]} {s[0].k.dtype}")
     r = np.ascontiguousarray(np.asarray(ranges, dtype=np.int64).reshape(-1, 3))
-    return r
-
-
-def _caches(caches):
-    """One cache or a list of them (one per layer) -> the C array, the number, the first."""
-    if isinstance(caches, _Pool):
-        return C.byref(caches.desc), 1, caches
-    n = len(caches)
-    return (type(caches[0].desc) * n)(*[c.desc for c in caches]), n, caches[0]
-
-
-def _row_shape(kv: KVCache):
-    return {torch.float32: ALORA_F32, torch.bfloat16: ALORA_BF16}[kv.k.dtype], int(kv.k.shape[1]), int(kv.k.shape[2])
-
-
-def _same_shape(x, y, shape_of):
-    if shape_of(x) != shape_of(y):
-        raise ValueError(f"caches of different shapes: {shape_of(x)} and {shape_of(y)}")
-
-
-def _q_shape(c):
-    return (int(c.k.shape[1]), c.head_dim) if isinstance(c, QCache) else (int(c.k.shape[1]), int(c.k.shape[2]))
+    kind = () if name == "alora_qcache_copy" else (_DTYPES[(d if typed == "dst" else s)[0].k.dtype],)
+    ctx._check(getattr(_lib, name)(ctx._h, *kind, *shapes[0], b"".join([bytes(c.desc) for c in d]), b"".join([bytes(c.desc) for c in s]), len(d),
+                                   _address(r), len(r), _stream_ptr(stream)))
 
 
 def alora_cache_copy(ctx: Context, dst, src, ranges, stream=None):
     """ranges [n, 3] of (source row, destination row, rows): pool rows of `src` to pool rows of `dst` (a KVCache, or a list of them, one per
     layer), as if every row had been read before any is written; dst and src may be the same caches."""
-    d, n, d0 = _caches(dst)
-    s, m, s0 = _caches(src)
-    _same_shape(d0, s0, _row_shape)
-    if n != m:
-        raise ValueError(f"{n} destination and {m} source layers")
-    r = _ranges(ranges)
-    dt, heads, h = _row_shape(d0)
-    ctx._check(_lib.alora_cache_copy(ctx._h, dt, heads, h, d, s, n, r.ctypes.data_as(C.POINTER(RowRange)), len(r), _stream_ptr(stream)))
+    _move("alora_cache_copy", ctx, dst, src, ranges, stream)
 
 
 def alora_qcache_copy(ctx: Context, dst, src, ranges, stream=None):
     """alora_cache_copy for QCaches."""
-    d, n, d0 = _caches(dst)
-    s, m, s0 = _caches(src)
-    _same_shape(d0, s0, _q_shape)
-    if n != m:
-        raise ValueError(f"{n} destination and {m} source layers")
-    r = _ranges(ranges)
-    heads, h = _q_shape(d0)
-    ctx._check(_lib.alora_qcache_copy(ctx._h, heads, h, d, s, n, r.ctypes.data_as(C.POINTER(RowRange)), len(r), _stream_ptr(stream)))
+    _move("alora_qcache_copy", ctx, dst, src, ranges, stream)
 
 
 def alora_qcache_store(ctx: Context, dst, src, ranges, stream=None):
     """Rows of KVCaches (src) into rows of 4 bits (dst): ranges as in alora_cache_copy."""
-    d, n, d0 = _caches(dst)
-    s, m, s0 = _caches(src)
-    _same_shape(d0, s0, _q_shape)
-    if n != m:
-        raise ValueError(f"{n} destination and {m} source layers")
-    r = _ranges(ranges)
-    ctx._check(_lib.alora_qcache_store(ctx._h, *_row_shape(s0), d, s, n, r.ctypes.data_as(C.POINTER(RowRange)), len(r), _stream_ptr(stream)))
+    _move("alora_qcache_store", ctx, dst, src, ranges, stream, typed="src")
 
 
 def alora_qcache_load(ctx: Context, dst, src, ranges, stream=None):
     """Rows of 4 bits (src) into rows of KVCaches (dst), exactly."""
-    d, n, d0 = _caches(dst)
-    s, m, s0 = _caches(src)
-    _same_shape(d0, s0, _q_shape)
-    if n != m:
-        raise ValueError(f"{n} destination and {m} source layers")
-    r = _ranges(ranges)
-    ctx._check(_lib.alora_qcache_load(ctx._h, *_row_shape(d0), d, s, n, r.ctypes.data_as(C.POINTER(RowRange)), len(r), _stream_ptr(stream)))
+    _move("alora_qcache_load", ctx, dst, src, ranges, stream, typed="dst")
 
 
 def alora_qcache_attend(ctx: Context, cache: QCache, q: torch.Tensor, cu_seqlens: Sequence[int], n_q_heads: int,
                         out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """q [T, n_q_heads * head_dim], rotated queries of the last rows of every sequence -> attention over the cache."""
     cu = _i32(cu_seqlens)
-    heads, h = _q_shape(cache)
+    h = cache.head_dim
     if out is None:
         out = torch.empty_like(q)
-    if q.dim() != 2 or q.shape[1] != n_q_heads * h or q.shape[0] != int(cu[-1]) or out.shape != q.shape or out.dtype != q.dtype:
+    if q.shape != (int(cu[-1]), n_q_heads * h) or out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError(f"q {tuple(q.shape)} and out {tuple(out.shape)} have to be [{int(cu[-1])}, {n_q_heads * h}] of one type")
-    dt = {torch.float32: ALORA_F32, torch.bfloat16: ALORA_BF16}[q.dtype]
-    ctx._check(_lib.alora_qcache_attend(ctx._h, dt, n_q_heads, heads, h, C.byref(cache.desc), _ptr(q), cu.ctypes.data_as(C.POINTER(C.c_int32)),
+    ctx._check(_lib.alora_qcache_attend(ctx._h, _DTYPES[q.dtype], n_q_heads, int(cache.k.shape[1]), h, C.byref(cache.desc), _ptr(q), _address(cu),
                                         len(cu) - 1, _ptr(out), _stream_ptr(stream)))
     return out
 
@@ -528,7 +502,7 @@ def _q_call(name, ctx, layers, caches, x, cu, k_per_seq, adapter_per_seq, out, w
     if out is None:
         out = torch.empty((x.shape[0], width), dtype=layers[0].dtype, device=layers[0].device)
     p = C.POINTER(C.c_int32)
-    descs = (QCacheDesc * len(caches))(*[c.desc for c in caches])
+    descs = b"".join([bytes(c.desc) for c in caches])
     args = [ctx._h, (LayerDesc * len(layers))(*[l.desc for l in layers])] + ([len(layers)] if stack else []) + [descs, _ptr(x)]
     if cu is not None:
         cu = _i32(cu)
