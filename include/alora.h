@@ -317,7 +317,7 @@ alora_status alora_lm_head(alora_ctx *ctx, alora_dtype dtype, int32_t d, int32_t
  * Format.  Row (token, kv head) has head_dim codes of 4 bits: a sign (bit 3) and a magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits
  * 2..0 = 0..7); element 2i is in the low half of byte i.  Each 32 channels of a head (the last block may be shorter) share one
  * exponent byte E: value = code * 2^(E - 127).  Storing takes E - 127 = e - 2 from the block's largest magnitude m * 2^e, 1 <= m < 2, or
- * e - 1 where m > 1.75 (at most a seventh of that magnitude is cut off), kept between -125 and 125, and rounds every channel to the
+ * e - 1 where m > 1.75 (at most a seventh of that magnitude is cut off), kept between -125 and 125, 0 for a block of zeros, and rounds every channel to the
  * nearest code, ties to the even one, magnitudes over 6 to 6.  Scales are powers of two, so a code depends on nothing but its
  * block's bits, and loading is exact in bf16 and fp32.  A block that holds a NaN or an infinity gets E = 255: all its values are NaN.
  * Other E outside [2, 252] are never stored; what attention makes of them is undefined. */

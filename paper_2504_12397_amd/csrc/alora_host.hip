@@ -1691,6 +1691,7 @@ struct QAttnPlan {
   QAttnClass cls[2];
   std::vector<int32_t> rows, counts;     // rows of the shared units; records per row, own and shared
   static size_t up(size_t b) { return (b + 15) & ~(size_t)15; }
+  size_t narrow_bytes() const { return cls[1].items.size() * sizeof(uint32_t); }      // (workspace: items that fp16 is too narrow for)
   size_t item_bytes() const { return up((cls[0].items.size() + cls[1].items.size()) * sizeof(QAttnItem)); }
   size_t bytes() const { return up(row_seq.size() * 4) + item_bytes() + up(rows.size() * 4) + up(counts.size() * 4); }
   void write(char *to) const {
@@ -1729,7 +1730,8 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
   const int nc_most = qt == Q_F32 ? 1 : ht == 256 ? 1 : qt == Q_F16 ? 2 : ht == 64 ? 4 : 2;
   struct Unit { int64_t row0; int len, first, n_rows, pos0; bool shared; };
   std::vector<Unit> units[2];
-  auto add = [&](const Unit &u) { units[(int64_t)u.n_rows * G > 16 ? 1 : 0].push_back(u); };
+  // (where a wave takes 16 columns at most, units of more are several of 16: one launch)
+  auto add = [&](const Unit &u) { units[nc_most > 1 && (int64_t)u.n_rows * G > 16 ? 1 : 0].push_back(u); };
   for (const SeqMeta &m : pl.seqs)
     if (m.n_new > 0) add(Unit{m.pool_off + m.prefix_len, m.P - m.prefix_len + m.n_new, m.row_start, m.n_new, m.P - m.prefix_len, false});
   if (pl.any_prefix) {
@@ -1754,7 +1756,7 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
     for (const Unit &u : units[k]) { cols = std::max(cols, (int64_t)u.n_rows * G); longest = std::max<int64_t>(longest, u.len); }
     c.nc = (int)std::min<int64_t>(nc_most, cols <= 16 ? 1 : cols <= 32 ? 2 : 4);
     const int waves = qattn_waves(ht);
-    while (c.cw < 4 && 16 * c.nc * c.cw < cols) c.cw *= 2;
+    while (k == 1 && c.cw < 4 && 16 * c.nc * c.cw < cols) c.cw *= 2;
     c.hw = waves / c.cw;
     while (c.hw > 1 && c.hw / 2 >= L.n_kv_heads) c.hw /= 2;
     const int slots = ctx->n_cu;
@@ -1773,6 +1775,8 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
     } else {
       for (int i = 0; i < 64 && r < longest && items_of(c.hw, r) > slots; ++i) r += std::max<int64_t>(32, r / 16);
     }
+    // (one row on 131072 keys: 256 records a head are merged in 9 us; half as many, with two waves on every head's keys, 46.9 -> 43.5 us, a quarter 45.5)
+    if (ctx->opt_splits == 0 && c.kr == 1 && c.hw == 8 && longest > 128 * r) { c.hw = 4; c.kr = 2; r *= 2; }
     r = std::min((r + 31) & ~(int64_t)31, (longest + 31) & ~(int64_t)31);
     range[k] = (int)r;
   }
@@ -1811,7 +1815,7 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
 }
 template <typename T>
 void run_qattn(alora_ctx *ctx, const QAttnPlan &q, const char *staged, const LayerDims &L, int T_rows, const QRows &rows, const SeqMeta *seqs_dev,
-               const void *Q, QueryType qt, float *partials, bool decode, T *out, hipStream_t s) {
+               const void *Q, QueryType qt, float *partials, uint32_t *narrow, bool decode, T *out, hipStream_t s) {
   const bool direct = q.n_parts == 1;
   MergeCounts mc{nullptr, 0};
   {
@@ -1835,9 +1839,14 @@ void run_qattn(alora_ctx *ctx, const QAttnPlan &q, const char *staged, const Lay
         if (n == 0) continue;
         a.hw = c.hw; a.kr = c.kr; a.cw = c.cw;
         const int ht = qattn_ht(L.head_dim);
-        if (qt == Q_BF16) launch_qattn_mfma_bf16(a, n, ht, c.nc, q.lds, s);
-        else if (qt == Q_F16) launch_qattn_mfma_f16(a, n, ht, c.nc, q.lds, s);
-        else launch_qattn_mfma_f32(a, n, ht, c.nc, q.lds, s);
+        // (fp16, and what was too narrow for it)
+        const bool half = q.lds && c.nc > 1 && qt != Q_F32;
+        a.narrow = half ? narrow : nullptr;
+        for (int pass = half ? 0 : 1; pass < 2; ++pass) {
+          if (qt == Q_BF16) launch_qattn_mfma_bf16(a, n, ht, c.nc, q.lds, pass == 0, s);
+          else if (qt == Q_F16) launch_qattn_mfma_f16(a, n, ht, c.nc, q.lds, pass == 0, s);
+          else launch_qattn_mfma_f32(a, n, ht, c.nc, q.lds, s);
+        }
         a.items += n;
       }
     }
@@ -1897,7 +1906,8 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   L.n_q = n_q_heads * head_dim; L.n_kv = n_kv_heads * head_dim; L.n_qkv = L.n_q + 2 * L.n_kv;
   const QueryType qt = dtype == ALORA_BF16 ? Q_BF16 : Q_F32;
   const QAttnPlan qp = plan_qattn(ctx, pl, L, qt, qattn_mfma_supported(ctx, L, *cache, q, out), qattn_lds_supported(L, *cache));
-  st = ensure_workspace(ctx, qp.n_parts > 1 ? attn_plain_partial_floats(L, pl.T, qp.n_parts) * sizeof(float) : 0);
+  const size_t partial_bytes = qp.n_parts > 1 ? (attn_plain_partial_floats(L, pl.T, qp.n_parts) * sizeof(float) + 255) & ~(size_t)255 : 0;
+  st = ensure_workspace(ctx, partial_bytes + qp.narrow_bytes());
   if (st != ALORA_OK) return st;
   const size_t seq_bytes = qp.mfma ? 0 : ((size_t)B * sizeof(SeqMeta) + 15) & ~(size_t)15;      // (the plain kernel reads the sequences' records)
   const size_t bytes = seq_bytes + qp.bytes();
@@ -1917,9 +1927,9 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   }
   const SeqMeta *seqs_dev = (const SeqMeta *)at;
   if (dtype == ALORA_BF16)
-    run_qattn<bf16>(ctx, qp, at + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, false, (bf16 *)out, s);
+    run_qattn<bf16>(ctx, qp, at + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, (uint32_t *)(ctx->ws + partial_bytes), false, (bf16 *)out, s);
   else
-    run_qattn<float>(ctx, qp, at + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, false, (float *)out, s);
+    run_qattn<float>(ctx, qp, at + seq_bytes, L, pl.T, rows_of(*cache), seqs_dev, q, qt, (float *)ctx->ws, (uint32_t *)(ctx->ws + partial_bytes), false, (float *)out, s);
   HIP_TRY(ctx, hipGetLastError());
   HIP_TRY(ctx, hipEventRecord(slot->ev, s));
   slot->in_flight = true;
@@ -2176,7 +2186,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   }
   // (caches of 4 bits: the new keys and values in the storage type, before they are stored)
   const size_t new_bytes = qc ? ((size_t)pl.T * L.n_kv * esz + 255) & ~(size_t)255 : 0;
-  st = ensure_workspace(ctx, probe.bytes + 2 * new_bytes);
+  st = ensure_workspace(ctx, probe.bytes + 2 * new_bytes + qp.narrow_bytes());
   if (st != ALORA_OK) return st;
   st = ensure_rope(ctx, pl.max_len, L.head_dim / 2, layers[0].rope_theta, s);
   if (st != ALORA_OK) return st;
@@ -2282,7 +2292,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     }
     const QueryForm qf = query_form<T>(ctx, L, w);
     run_qattn<T>(ctx, qp, slot->dev + q_at + qseq_bytes, L, pl.T, rows_of(qc[l]), (const SeqMeta *)(slot->dev + q_at), w.Q, qf.half ? Q_F16 : Q_F32, w.partials,
-                 decode, attn, s);
+                 (uint32_t *)(ctx->ws + probe.bytes + 2 * new_bytes), decode, attn, s);
   };
   if (qc && !stack) {
     if (bf) q_block(0, (const bf16 *)x, (bf16 *)out);

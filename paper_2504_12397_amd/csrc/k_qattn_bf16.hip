@@ -3,12 +3,15 @@
 
 namespace alora {
 
-void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s) {
-  if (lds && ht == 64 && nc == 4) return qattn_lds_start<64, 1, 2, 4, 4, 2, bf16, bf16>(a, n_items, s);
-  if (lds && ht == 64 && nc == 2) return qattn_lds_start<64, 1, 2, 2, 5, 2, bf16, bf16>(a, n_items, s);
-  if (lds && ht == 64 && nc == 1) return qattn_lds_start<64, 1, 2, 1, 3, 4, bf16, bf16>(a, n_items, s);
-  if (lds && ht == 128 && nc == 2) return qattn_lds_start<128, 1, 2, 2, 4, 2, bf16, bf16>(a, n_items, s);
-  if (lds && ht == 128 && nc == 1) return qattn_lds_start<128, 1, 2, 1, 2, 4, bf16, bf16>(a, n_items, s);
+void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, bool half, hipStream_t s) {
+  if (lds && half && ht == 64 && nc == 4) return qattn_lds_start<64, 1, 2, 4, 4, 2, true, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 64 && nc == 4) return qattn_lds_start<64, 1, 2, 4, 4, 2, false, bf16, bf16>(a, n_items, s);
+  if (lds && half && ht == 64 && nc == 2) return qattn_lds_start<64, 1, 2, 2, 5, 2, true, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 64 && nc == 2) return qattn_lds_start<64, 1, 2, 2, 5, 2, false, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 64 && nc == 1) return qattn_lds_start<64, 1, 2, 1, 3, 4, false, bf16, bf16>(a, n_items, s);
+  if (lds && half && ht == 128 && nc == 2) return qattn_lds_start<128, 1, 2, 2, 4, 2, true, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 128 && nc == 2) return qattn_lds_start<128, 1, 2, 2, 4, 2, false, bf16, bf16>(a, n_items, s);
+  if (lds && ht == 128 && nc == 1) return qattn_lds_start<128, 1, 2, 1, 2, 4, false, bf16, bf16>(a, n_items, s);
   if (!lds && ht == 64 && nc == 4) return qattn_mfma_start<64, 1, 2, 4, 1, bf16, bf16>(a, n_items, s);
   if (!lds && ht == 64 && nc == 2) return qattn_mfma_start<64, 1, 2, 2, 3, bf16, bf16>(a, n_items, s);
   if (!lds && ht == 64 && nc == 1) return qattn_mfma_start<64, 1, 2, 1, 4, bf16, bf16>(a, n_items, s);

@@ -103,11 +103,11 @@ void launch_rows_copy_ordered(const RowsOrderedArgs &a, hipStream_t s) {
 
 // ---- rows of the storage type <-> rows of 4 bits -------------------------------------------------------------
 // The exponent byte of a block with this largest magnitude (as bits): that of the magnitude less 2, so that it lands in [4, 8) of the
-// codes' [0, 6]; less 1 where its mantissa is over 1.75, so that at most a seventh of the magnitude is cut off (7 -> 6).
+// codes' [0, 6]; less 1 where its mantissa is over 1.75, so that at most a seventh of the magnitude is cut off (7 -> 6).  Blocks of zeros have 127.
 __device__ __forceinline__ int q_exponent(uint32_t amax_bits) {
   if (amax_bits >= 0x7f800000u) return Q_E_NAN;
   const int e = (int)((amax_bits + 0x1fffffu) >> 23) - 2;
-  return min(max(e, Q_E_MIN), Q_E_MAX);
+  return amax_bits == 0 ? 127 : min(max(e, Q_E_MIN), Q_E_MAX);
 }
 __device__ __forceinline__ float q_scale(int e) { return __builtin_bit_cast(float, (uint32_t)e << 23); }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }

@@ -11,8 +11,12 @@
 //     one channel of two keys side by side, which is the transposition: product c is channel CPL i + c of lane row i.
 // No LDS and no barrier but where several waves share a head's keys (KR > 1): they join at the end, in pairs.
 // Queries of bf16 are one operand, exactly; fp16 two (high and low bits as bf16), fp32 three.  Probabilities are two operands (16 bits; one of 8
-// bits would add half of what the rounding of a bf16 result does), three for fp32.
-// The reference exponent of a column moves only when a score exceeds it by 2^8: almost no step rescales the sums.
+// bits would add half of what the rounding of a bf16 result does), three for fp32.  Units of many columns, where the products count and not memory, take one operand
+// of fp16 (11 bits) with values of fp16, as long as that holds them exactly: a workgroup looks at the smallest exponent that it met and at whether its sums
+// are numbers, and says so where fp16 was too narrow; a second launch does those items, and no others, with operands of bf16.  128 rows of 32 heads on 32896 keys
+// 139 -> 120 us, the second launch (4 us) included.
+// The reference exponent of a column moves only when a score exceeds it by 2^8 more than it did: almost no step rescales the sums.  It begins 8 above the largest score
+// so far, so that probabilities are 1 at most (values may be as large as fp32 holds); in fp16 7 below it, for the sake of that type's small numbers: 2^15 at most.
 #pragma once
 #include "lds_dma.h"
 #include "qcache.h"
@@ -23,8 +27,10 @@ typedef __bf16 qa_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 qa_bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t qa_u32x4 __attribute__((ext_vector_type(4)));
 typedef float qa_f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 qa_f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 qa_f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr float QA_LAZY = 8.0f;      // log2 units
+constexpr uint32_t QA_F16_FIRST = 114;      // the first exponent byte whose smallest value, 0.5 * 2^(E - 127), is a normal number of fp16
 
 // byte b of w: two codes, as a pair of bf16
 __device__ __forceinline__ uint32_t qa_pair(uint32_t w, float scale, int b) {
@@ -34,6 +40,16 @@ __device__ __forceinline__ uint32_t qa_pair(uint32_t w, float scale, int b) {
     case 1: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1); break;
     case 2: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2); break;
     default: r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  }
+  return __builtin_bit_cast(uint32_t, r);
+}
+__device__ __forceinline__ uint32_t qa_pair16(uint32_t w, float scale, int b) {      // as a pair of fp16
+  qa_f16x2 r;
+  switch (b) {
+    case 0: r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0); break;
+    case 1: r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1); break;
+    case 2: r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2); break;
+    default: r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
   }
   return __builtin_bit_cast(uint32_t, r);
 }
@@ -73,6 +89,7 @@ struct QaWork {
   bool active, shared;
   int col0, n_cols;              // its columns
   int kbeg, kend, see_all;       // its keys; keys below see_all are seen by every column
+  int steps;                     // of 32 keys that a wave of the workgroup takes at most
   int64_t key_row0;
   int first_row, pos0, part;
 };
@@ -90,6 +107,7 @@ template <int NC> __device__ __forceinline__ QaWork qa_work(const QAttnArgs &a, 
   const int last_tok = (w.col0 + max(w.n_cols, 1) - 1) / G, first_tok = w.col0 / G;
   int per = (it.kend - it.kbeg + a.kr - 1) / a.kr;
   per = (per + 31) & ~31;
+  w.steps = per >> 5;
   w.kbeg = it.kbeg + w.sub * per;
   w.kend = min(it.kend, w.kbeg + per);
   if (!it.shared) w.kend = min(w.kend, it.pos0 + last_tok + 1);
@@ -112,14 +130,17 @@ template <int HT> struct QaTile {
 };
 
 // The columns of a wave: queries, running sums, and what is done with 32 keys.
-template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColumns {
+// HALF: probabilities and values as fp16.
+template <int HT, int NQ, int NP, int NC, bool HALF, typename TQ, typename T> struct QaColumns {
   typedef QaTile<HT> Tile;
+  static constexpr float ABOVE = HALF ? -7.f : 8.f, LAZY = HALF ? 15.f : 0.f;      // log2 units: where a new reference lies, how far a score may exceed it
   static constexpr int KS = Tile::KS, CPL = Tile::CPL, VW = Tile::VW, KSC = Tile::KSC;
   uint32_t qf[NC][NQ][KS][4];
   int lim[NC];                            // last key that the column sees
   qa_f32x4 o[NC][CPL];                    // o[c][v] of lane (j, kg): channel CPL * (4 kg + v) + c of column j
   float m_ref[NC], neg_m[NC], l[NC];      // reference exponent (log2), its negative or 0 where there is none, this lane's part of the sum
   uint32_t nan_blocks[NC];                // blocks of 32 channels in which the column has met a value that is not a number
+  uint32_t e_min;                         // HALF: the smallest exponent of a value so far
   int j, kg;
   float c_scale;
 
@@ -168,6 +189,19 @@ template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColu
       neg_m[nc] = l[nc] = 0.f;
       nan_blocks[nc] = 0;
     }
+    e_min = 255;
+  }
+
+  // Some value was too small for fp16, or too large (the sums are infinite or no numbers; or they would be so anyway).
+  __device__ __forceinline__ bool too_narrow() const {
+    float z = 0.f;
+#pragma unroll
+    for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) z += o[nc][c][v] - o[nc][c][v];
+    return e_min < QA_F16_FIRST || !(z == 0.f);
   }
 
   // 32 keys from k0 on.  k_used() is called once t.k has been read, need_v() before t.v is, v_used() after.
@@ -195,13 +229,16 @@ template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColu
     k_used();
     need_v();
     if (k0 + 32 > w.see_all) {      // a step that some column sees in part
+      int first = k0 + 4 * kg;
+      asm volatile("" : "+v"(first));      // (the comparisons stay here: made ahead of the branch they cost every step 17 instructions and as many pairs of registers)
       bool bad = false;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const int key = k0 + 16 * u + 4 * kg + v;
+          const int key = first + 16 * u + v;
           bad |= t.vs[u][v] == (uint32_t)Q_E_NAN;
+          if (HALF && key >= w.kend) t.vs[u][v] = 127;      // (rows that are not there read as zeros, whose exponent is no concern)
 #pragma unroll
           for (int nc = 0; nc < NC; ++nc)
             if (key >= w.kend || key > lim[nc]) sc[nc][u][v] = -INFINITY;
@@ -214,7 +251,7 @@ template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColu
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const int key = k0 + 16 * u + 4 * kg + v;
+            const int key = first + 16 * u + v;
             const uint8_t *sp = scales + (int64_t)min(key, w.kend - 1) * a.n_kv_heads * nb;
             uint32_t blocks = 0;
             for (int b = 0; b < nb; ++b) blocks |= (sp[b] == Q_E_NAN ? 1u : 0u) << b;
@@ -229,15 +266,16 @@ template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColu
           }
       }
     }
-    uint32_t pf[NC][NP][4];
+    constexpr int PP = HALF ? 1 : NP;
+    uint32_t pf[NC][PP][4];
 #pragma unroll
     for (int nc = 0; nc < NC; ++nc) {
       float mx = sc[nc][0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) mx = fmaxf(mx, sc[nc][i >> 2][i & 3]);
       mx *= c_scale;
-      if (__any(mx > m_ref[nc] + QA_LAZY)) {
-        const float m_new = fmaxf(m_ref[nc], qa_max4(mx)), neg_new = m_new == -INFINITY ? 0.f : -m_new;
+      if (__any(mx > m_ref[nc] + LAZY)) {
+        const float m_new = fmaxf(m_ref[nc], qa_max4(mx) + ABOVE), neg_new = m_new == -INFINITY ? 0.f : -m_new;
         const float alpha = __builtin_amdgcn_exp2f(m_ref[nc] + neg_new);
         m_ref[nc] = m_new;
         neg_m[nc] = neg_new;
@@ -250,9 +288,22 @@ template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColu
       float p[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(sc[nc][i >> 2][i & 3], c_scale, neg_m[nc]));
-      l[nc] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      if constexpr (HALF) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) qa_split<NP>(p[2 * i], p[2 * i + 1], &pf[nc][0][i], 4);
+        for (int i = 0; i < 4; ++i) {      // (the sum is of the rounded probabilities: numerator and denominator carry the same rounding)
+          const qa_f16x2 w = {(_Float16)p[2 * i], (_Float16)p[2 * i + 1]};
+          pf[nc][0][i] = __builtin_bit_cast(uint32_t, w);
+          l[nc] = __builtin_amdgcn_fdot2(w, qa_f16x2{(_Float16)1.f, (_Float16)1.f}, l[nc], false);
+        }
+      } else {
+        l[nc] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qa_split<NP>(p[2 * i], p[2 * i + 1], &pf[nc][0][i], 4);
+      }
+    }
+    if constexpr (HALF) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e_min = min(e_min, t.vs[i >> 2][i & 3]);
     }
     float ev[2][4];
 #pragma unroll
@@ -263,7 +314,10 @@ template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColu
     for (int c2 = 0; c2 < CPL / 2; ++c2) {
       uint32_t e[8];      // channels 2 c2 and 2 c2 + 1 of the lane's eight keys
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = qa_pair(t.v[i >> 2][i & 3][c2 / 4], ev[i >> 2][i & 3], c2 & 3);
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t c = t.v[i >> 2][i & 3][c2 / 4];
+        e[i] = HALF ? qa_pair16(c, ev[i >> 2][i & 3], c2 & 3) : qa_pair(c, ev[i >> 2][i & 3], c2 & 3);
+      }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const uint32_t sel = half ? 0x07060302u : 0x05040100u;
@@ -273,9 +327,11 @@ template <int HT, int NQ, int NP, int NC, typename TQ, typename T> struct QaColu
 #pragma unroll
         for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
-          for (int p = 0; p < NP; ++p) {
+          for (int p = 0; p < PP; ++p) {
             const qa_u32x4 pv = {pf[nc][p][0], pf[nc][p][1], pf[nc][p][2], pf[nc][p][3]};
-            o[nc][2 * c2 + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(qa_bf16x8, vf), __builtin_bit_cast(qa_bf16x8, pv), o[nc][2 * c2 + half], 0, 0, 0);
+            qa_f32x4 &to = o[nc][2 * c2 + half];
+            if constexpr (HALF) to = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(qa_f16x8, vf), __builtin_bit_cast(qa_f16x8, pv), to, 0, 0, 0);
+            else to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(qa_bf16x8, vf), __builtin_bit_cast(qa_bf16x8, pv), to, 0, 0, 0);
           }
       }
     }
@@ -437,7 +493,7 @@ __global__ __launch_bounds__(64 * qattn_waves(HT), HT == 256 ? 1 : 2) void qattn
   Tile ring[DEPTH];
 #pragma unroll
   for (int d = 0; d < DEPTH; ++d) { load_k(ring[d], w.kbeg + 32 * d); load_v(ring[d], w.kbeg + 32 * d); }
-  QaColumns<HT, NQ, NP, NC, TQ, T> q;
+  QaColumns<HT, NQ, NP, NC, false, TQ, T> q;
   q.begin(a, w, lane);
   for (int k0 = w.kbeg; k0 < w.kend; k0 += 32 * DEPTH) {
 #pragma unroll
@@ -465,8 +521,10 @@ __device__ __forceinline__ void qa_dword_to_lds(i32x4 rsrc, int voff, int lds) {
   lds = __builtin_amdgcn_readfirstlane(lds);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
 }
-template <int HT, int NQ, int NP, int NC, int DEPTH, int OCC, typename TQ, typename T>
+// OCC: waves on a SIMD.
+template <int HT, int NQ, int NP, int NC, int DEPTH, int OCC, bool HALF, typename TQ, typename T>
 __global__ __launch_bounds__(512, OCC) void qattn_lds_kernel(QAttnArgs a) {
+  if (!HALF && a.narrow != nullptr && a.narrow[blockIdx.x] == 0) return;      // (done in fp16)
   typedef QaTile<HT> Tile;
   typedef QaRing<HT, DEPTH> R;
   extern __shared__ __align__(16) char s_ring[];
@@ -508,7 +566,7 @@ __global__ __launch_bounds__(512, OCC) void qattn_lds_kernel(QAttnArgs a) {
   };
 #pragma unroll
   for (int d = 0; d < DEPTH; ++d) ask(w.kbeg + 32 * d, d);
-  QaColumns<HT, NQ, NP, NC, TQ, T> q;
+  QaColumns<HT, NQ, NP, NC, HALF, TQ, T> q;
   q.begin(a, w, lane);
   // the queries are here before the first step (a wait for them inside the loop would be one for everything on the way)
 #pragma unroll
@@ -525,11 +583,13 @@ __global__ __launch_bounds__(512, OCC) void qattn_lds_kernel(QAttnArgs a) {
   const int v_at = R::ROWS + kg * hb + j * Tile::VB;      // slot of row 16 u + 4 kg + n: 16 u + 4 n + kg
   const int vs_at = 2 * R::ROWS + 256 + 16 * kg + e_in + Tile::CPL * j / QBLOCK;
   int slot = 0;
-  for (int k0 = w.kbeg; k0 < w.kend; k0 += 32) {
-    wait_vm<(DEPTH - 1) * R::PER_STEP>();
+  for (int i = 0; i < w.steps; ++i) {
     // The heads of a token share lines of memory: waves that drift apart fetch them twice (64 x 16449 keys: 1.29 GB instead of 1.15, 248 us; so 206).
-    // (Waves of a workgroup have different numbers of steps where they share keys, and join through barriers there: not then.)
-    if (a.kr == 1) __builtin_amdgcn_s_barrier();
+    // Every wave of the workgroup comes by here as often as the others.
+    __builtin_amdgcn_s_barrier();
+    const int k0 = w.kbeg + 32 * i;
+    if (k0 >= w.kend) continue;
+    wait_vm<(DEPTH - 1) * R::PER_STEP>();
     const char *st = ring + slot * R::STAGE;
     Tile t;
 #pragma unroll
@@ -559,6 +619,18 @@ __global__ __launch_bounds__(512, OCC) void qattn_lds_kernel(QAttnArgs a) {
     slot = slot + 1 == DEPTH ? 0 : slot + 1;
   }
   wait_vm<0>();      // (nothing of this wave may land in LDS that is another's by then)
+  if constexpr (HALF) {
+    __syncthreads();      // (every wave is through with its ring)
+    int *said = reinterpret_cast<int *>(s_ring);
+    const bool narrow = __any(q.too_narrow());
+    if (lane == 0) said[wave] = narrow;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int any = 0;
+      for (int i = 0; i < 8; ++i) any |= said[i];
+      a.narrow[blockIdx.x] = (uint32_t)any;
+    }
+  }
   if (a.kr > 1) {
     __syncthreads();
     q.join(a, w, wave % a.hw, lane, reinterpret_cast<float *>(s_ring));
@@ -575,9 +647,9 @@ void qattn_mfma_start(const QAttnArgs &a, int n_items, hipStream_t s) {
   if (smem > 48 * 1024) (void)hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   hipLaunchKernelGGL(kern, dim3(n_items), dim3(64 * W), smem, s, a);
 }
-template <int HT, int NQ, int NP, int NC, int DEPTH, int OCC, typename TQ, typename T>
+template <int HT, int NQ, int NP, int NC, int DEPTH, int OCC, bool HALF, typename TQ, typename T>
 void qattn_lds_start(const QAttnArgs &a, int n_items, hipStream_t s) {
-  auto kern = qattn_lds_kernel<HT, NQ, NP, NC, DEPTH, OCC, TQ, T>;
+  auto kern = qattn_lds_kernel<HT, NQ, NP, NC, DEPTH, OCC, HALF, TQ, T>;
   const size_t join = a.kr == 1 ? 0 : (size_t)4 * NC * (HT / 4 + 3) * 64 * sizeof(float), ring = (size_t)8 * QaRing<HT, DEPTH>::WAVE;
   const size_t smem = join > ring ? join : ring;
   static_assert(8 * QaRing<HT, DEPTH>::WAVE <= 160 * 1024 && 4 * NC * (HT / 4 + 3) * 256 <= 160 * 1024, "");

@@ -91,11 +91,13 @@ struct QAttnArgs {
   float sm_scale;
   float *partials;          // [T, n_q_heads, n_parts, head_dim + 2] (sums, maximum, sum of probabilities), used when out == nullptr
   void *out;                // [T, n_q_heads, head_dim], with n_parts == 1 only
+  uint32_t *narrow;         // [items] or nullptr: written by a launch in fp16, 1 where that was too narrow; the launch after it does those items
 };
 // ht: 64, 128 or 256, the smallest that holds head_dim.  Codes begin at multiples of 4 bytes, queries and results of 16.
 // lds: head_dim is 64 (with an even number of kv heads) or 128, codes begin at multiples of 16 bytes and exponents at multiples of 4.
-void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s);      // queries of bf16; nc 1, 2 or 4 (ht 256: 1, 2)
-void launch_qattn_mfma_f16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s);       // of fp16; nc 1 or 2 (ht 256: 1)
-void launch_qattn_mfma_f32(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s);       // of fp32; nc 1
+// half: fp16 (lds and nc > 1 only); otherwise, with args.narrow, only items that are marked there.
+void launch_qattn_mfma_bf16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, bool half, hipStream_t s);      // queries of bf16; nc 1, 2 or 4 (ht 128: 1, 2; 256: 1)
+void launch_qattn_mfma_f16(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, bool half, hipStream_t s);       // of fp16; nc 1 or 2 (ht 256: 1)
+void launch_qattn_mfma_f32(const QAttnArgs &a, int n_items, int ht, int nc, bool lds, hipStream_t s);                  // of fp32; nc 1
 
 }  // namespace alora

@@ -20,7 +20,7 @@ def quantise(x):
         top = np.abs(b).max(-1)
         m, e = np.frexp(top)                        # top = 2 m * 2^(e - 1)
         ex = np.where(2 * m > 1.75, e - 1 - 1, e - 1 - 2)
-        ex = np.clip(np.where(top == 0, -125, ex), -125, 125)
+        ex = np.where(top == 0, 0, np.clip(ex, -125, 125))
         y = np.abs(b) / np.exp2(ex)[..., None]
         level = np.zeros(b.shape, dtype=np.int64)
         for i, t in enumerate(MIDS):                # a tie goes to the even code
@@ -42,10 +42,10 @@ def values(codes, exps):
 
 def attend(q, K, V, n_q_heads, visible):
     """q [S, n_q_heads * h]; K, V [L, n_kv, h] of one sequence; row i sees the first visible[i] keys.  Returns the result and, for its error:
-    sum_j p_j |v_j| and max_j sum_c |q_c k_jc| / sqrt(h), elementwise and per (row, head)."""
+    sum_j p_j |v_j|, sum_j |v_j| (elementwise) and max_j sum_c |q_c k_jc| / sqrt(h) (per row and head)."""
     L, n_kv, h = K.shape
     G = n_q_heads // n_kv
-    out, mag = np.empty(q.shape), np.empty(q.shape)
+    out, mag, total = np.empty(q.shape), np.empty(q.shape), np.empty(q.shape)
     spread = np.empty((q.shape[0], n_q_heads))
     for i in range(q.shape[0]):
         n = visible[i]
@@ -56,16 +56,18 @@ def attend(q, K, V, n_q_heads, visible):
             p /= p.sum()
             out[i, j * h:(j + 1) * h] = p @ v
             mag[i, j * h:(j + 1) * h] = p @ np.abs(v)
+            total[i, j * h:(j + 1) * h] = np.abs(v).sum(0)
             spread[i, j] = (np.abs(k) @ np.abs(qv)).max() / np.sqrt(h)
-    return out, mag, spread
+    return out, mag, total, spread
 
 
-def tolerance(ref, mag, spread, h, L, dtype):
+def tolerance(ref, mag, total, spread, h, L, dtype):
     """|result - ref| is at most
       half a step of the stored type, plus mag = sum p |v| times
       2 * (error of a score): h + 8 fp32 roundings of the terms of q k / sqrt(h), times their sum (spread), its square-root scale included,
           and 2^-22 * spread for the exponent's argument (score less maximum, both at most 1.45 spread in base 2);
-      2 * 2^-16: a probability carried in 16 bits (bf16) or more, numerator and denominator;
+      2 * 2^-11 (bf16): a probability rounded to the 11 bits of fp16, at most half a step, in the numerator and the denominator; fp32: 2 * 2^-21, 24 bits and the exponential's own error;
+          and what fp16 loses of small ones: half of its smallest number, 2^-25, where the largest probability is 2^7 or more: 2^-32 of sum |v|;
       2 * (L / 8 + 64) * 2^-24: the running sums over keys, eight terms or more at a time, and the joining of partial ones."""
-    c = 2 * ((h + 8) * 2.0 ** -24 + 2.0 ** -22) * np.repeat(spread, h, axis=-1) + 2 * 2.0 ** (-16 if dtype == "bf16" else -21) + 2 * (L / 8 + 64) * 2.0 ** -24
-    return HALF[dtype] * np.abs(ref) + c * mag + 1e-37
+    c = 2 * ((h + 8) * 2.0 ** -24 + 2.0 ** -22) * np.repeat(spread, h, axis=-1) + 2 * 2.0 ** (-11 if dtype == "bf16" else -21) + 2 * (L / 8 + 64) * 2.0 ** -24
+    return HALF[dtype] * np.abs(ref) + c * mag + (2.0 ** -32 * total if dtype == "bf16" else 0.0) + 1e-37

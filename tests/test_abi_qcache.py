@@ -228,12 +228,13 @@ def test_format_by_hand():
     assert codes[0] == 7 | (0 << 4) and codes[2] == 2 | ((8 | 4) << 4)      # element 0 low, element 1 high; -2 is code 4 with the sign
     assert list(qref.quantise(np.array([7.01, 1.0]))[1]) == [128]
     assert list(qref.quantise(np.array([np.nan, 1.0]))[1]) == [255] and list(qref.quantise(np.array([1e-45, 0.0]))[1]) == [2]
+    assert list(qref.quantise(np.array([0.0, -0.0]))[1]) == [127]
     assert list(qref.quantise(np.array([3.4e38, 0.0]))[1]) == [252]
 
 
 def test_attention_by_hand():
     K = np.array([[[1.0, 0.0]], [[0.0, 1.0]]])
     V = np.array([[[2.0, 0.0]], [[0.0, 4.0]]])
-    out, _, _ = qref.attend(np.array([[0.0, 0.0], [np.log(3.0) * np.sqrt(2.0), 0.0]]), K, V, 1, [2, 2])
+    out = qref.attend(np.array([[0.0, 0.0], [np.log(3.0) * np.sqrt(2.0), 0.0]]), K, V, 1, [2, 2])[0]
     assert np.allclose(out, [[1.0, 2.0], [1.5, 1.0]])
     assert np.allclose(qref.attend(np.array([[5.0, 1.0]]), K, V, 1, [1])[0], [[2.0, 0.0]])

@@ -82,8 +82,8 @@ class Batch:
         for b in range(len(self.own)) if only is None else only:
             if self.new[b] == 0:
                 continue
-            ref, mag, spread = self.reference(b)
-            tol = qref.tolerance(ref, mag, spread, self.h, len(self.rows(b)), self.dtype)
+            ref, mag, total, spread = self.reference(b)
+            tol = qref.tolerance(ref, mag, total, spread, self.h, len(self.rows(b)), self.dtype)
             err = np.abs(out[self.cu[b]:self.cu[b + 1]] - ref)
             assert np.isfinite(err).all(), f"sequence {b}: not finite"
             worst = max(worst, float((err / tol).max()))
@@ -150,6 +150,22 @@ def test_exponents_of_every_size(ab, ctx, e_k, e_v):
         b.q, b.q64 = q.cuda(), q.double().numpy()
         b.cache = b.make(ab)
         b.check(ab.alora_qcache_attend(ctx, b.cache, b.q, b.cu, 4))
+
+
+@pytest.mark.parametrize("e_v", [113, 114, 139, 140, 141, 90, 160])
+@pytest.mark.parametrize("h", [64, 128])
+def test_values_around_what_fp16_holds(ab, ctx, h, e_v):
+    """Units of many columns multiply in fp16 where it holds the values: exponents on both sides of that, in all rows and in one block of one row, zeros between."""
+    for everywhere in (True, False):
+        b = Batch(ab, "bf16", 8, 2, h, [300, 45], [40, 45], C=[130], group=[0, -1], seed=17)
+        c, e = b.codes[1]
+        c[b.rows(0)[7:20]] = 0
+        if everywhere:
+            e[e != 255] = e_v
+        else:
+            e[b.rows(0)[211], 1, 1] = e_v
+        b.cache = b.make(ab)
+        b.check(ab.alora_qcache_attend(ctx, b.cache, b.q, b.cu, 8))
 
 
 @pytest.mark.parametrize("dtype,n_q,n_kv,h", [("bf16", 8, 2, 128), ("f32", 4, 4, 64), ("bf16", 8, 2, 64), ("bf16", 4, 2, 256), ("bf16", 10, 5, 80)])
@@ -300,7 +316,7 @@ def check_layers(ab, ctx, case, four, full, out, decode):
         at = np.arange(n) + int(four.seq_offset[b]) - plen
         if plen:
             at[:plen] = np.arange(plen) + int(four.prefix_offset[b])
-        want, _, _ = qref.attend(q, K[at], V[at], shape.n_q_heads, list(pos + 1))
+        want = qref.attend(q, K[at], V[at], shape.n_q_heads, list(pos + 1))[0]
         e = H.rel_err(H.f64(out[case.cu[b]:case.cu[b + 1]]), want)
         worst = max(worst, e)
         assert e <= tol, f"sequence {b}: {e:.3e}"
