@@ -344,7 +344,8 @@ typedef struct { int64_t src, dst, n; } alora_row_range;
  *   dst, src  HOST [n_layers]: caches of one shape (dtype, n_kv_heads, head_dim); pools may differ in size, each is the same in all layers
  *   ranges    HOST [n_ranges]; rows outside a pool: ALORA_ECAPACITY; destination ranges that overlap each other, negative n: ALORA_EINVAL.
  *             n = 0 is allowed, and n_ranges = 0 is a valid no-op.
- * dst[l] and src[l] are the same arrays or do not overlap in memory (ALORA_EINVAL where bases differ and memory overlaps).  Rows that move
+ * dst[l] and src[l] are the same arrays or do not overlap in memory (ALORA_EINVAL where bases differ and memory overlaps); arrays of different layers, and
+ * keys and values, never overlap.  Rows that move
  * over others, some towards the front and some towards the back, are staged through the context's workspace. */
 alora_status alora_cache_copy(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_kv_cache *dst,
                               const alora_kv_cache *src, int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
@@ -364,8 +365,8 @@ alora_status alora_qcache_load(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads
  *   q          DEVICE [T, n_q_heads * head_dim] (dtype): rotated queries, sequences back to back
  *   cu_seqlens HOST [B+1] as in alora_prefill.  The S_b rows of sequence b are the last S_b of its seq_len[b] cached positions, all of them in its own
  *              rows (S_b <= seq_len[b] - prefix_len[b]): row i sees positions 0 .. seq_len[b] - S_b + i.  S_b = 0 leaves a sequence alone.
- *   out        DEVICE [T, n_q_heads * head_dim] (dtype)
- * softmax(q k / sqrt(head_dim)) v with queries, keys and values as they are (no rounding), sums in fp32.  A NaN in a key or value reaches the
+ *   out        DEVICE [T, n_q_heads * head_dim] (dtype), apart from q (ALORA_EINVAL where they overlap)
+ * softmax(q k / sqrt(head_dim)) v with queries, keys and values as they are, sums in fp32; results of bf16 may come from probabilities of 11 bits (fp16).  A NaN in a key or value reaches the
  * rows that see its position and no others.  Sequences of the call may name the same rows.  Prefixes that several sequences name are walked once for all of
  * them.  Errors as everywhere; under capture into a HIP graph ALORA_EINVAL (the call stages its work list from the host). */
 alora_status alora_qcache_attend(alora_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *cache,

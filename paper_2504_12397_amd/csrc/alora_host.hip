@@ -1526,7 +1526,7 @@ alora_status copy_rows_ordered(alora_ctx *ctx, const RowJob &job, const std::vec
     if (ctx->flags) HIP_TRY(ctx, hipFree(ctx->flags));
     ctx->flags = nullptr;
     ctx->flags_cap = 0;
-    const size_t cap = std::max<size_t>(4096, want + want / 2);
+    const size_t cap = std::max<size_t>(tickets + (1 << 17), want + want / 2);
     HIP_TRY(ctx, hipMalloc((void **)&ctx->flags, cap * sizeof(uint32_t)));
     HIP_TRY(ctx, hipMemset(ctx->flags, 0, cap * sizeof(uint32_t)));
     ctx->flags_cap = cap;
@@ -1539,25 +1539,33 @@ alora_status copy_rows_ordered(alora_ctx *ctx, const RowJob &job, const std::vec
     HIP_TRY(ctx, hipDeviceSynchronize());
     ctx->flags_epoch = 1;
   }
+  RowsOrderedArgs a{nullptr, nullptr, (int)steps.size(), (int)planes.size(), 0, ctx->flags, ctx->flags + tickets, ctx->flags_epoch};
+  RowsFew few{};
   const size_t sb = steps.size() * sizeof(RowStep), pb = (planes.size() * sizeof(RowPlane) + 15) & ~(size_t)15;
   MetaSlot *slot = nullptr;
-  const alora_status got = acquire_slot(ctx, sb + pb, &slot);
-  if (got != ALORA_OK) return got;
-  memcpy(slot->host, steps.data(), sb);
-  memcpy(slot->host + sb, planes.data(), planes.size() * sizeof(RowPlane));
-  const char *at = slot->host;      // short lists are read where they are
-  if (sb + pb > 16384) {
+  if (sb + pb <= ROWS_FEW_BYTES) {
+    a.planes_at = (int)sb;
+    memcpy(few.data, steps.data(), sb);
+    memcpy(few.data + sb, planes.data(), planes.size() * sizeof(RowPlane));
+  } else {
+    const alora_status got = acquire_slot(ctx, sb + pb, &slot);
+    if (got != ALORA_OK) return got;
+    memcpy(slot->host, steps.data(), sb);
+    memcpy(slot->host + sb, planes.data(), planes.size() * sizeof(RowPlane));
     const int n16 = (int)((sb + pb) / 16);
     hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
-    at = slot->dev;
+    a.steps = (const RowStep *)slot->dev;
+    a.planes = (const RowPlane *)(slot->dev + sb);
   }
   {
     ProfScope p(ctx, K_ROWS, s);
-    launch_rows_copy_ordered(RowsOrderedArgs{(const RowStep *)at, (const RowPlane *)(at + sb), (int)steps.size(), (int)planes.size(), ctx->flags, ctx->flags + tickets, ctx->flags_epoch}, s);
+    launch_rows_copy_ordered(a, few, s);
   }
   HIP_TRY(ctx, hipGetLastError());
-  HIP_TRY(ctx, hipEventRecord(slot->ev, s));
-  slot->in_flight = true;
+  if (slot) {
+    HIP_TRY(ctx, hipEventRecord(slot->ev, s));
+    slot->in_flight = true;
+  }
   *done = true;
   return ALORA_OK;
 }
@@ -1661,7 +1669,7 @@ alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_di
   HIP_TRY(ctx, hipSetDevice(ctx->device));
   std::vector<RowPlane> planes;
   planes.reserve((size_t)2 * n_layers);
-  bool wide = head_dim % QBLOCK == 0;
+  bool wide = head_dim % 8 == 0;
   for (int l = 0; l < n_layers; ++l)
     for (int v = 0; v < 2; ++v) {
       void *f = v ? full[l].v : full[l].k, *q = v ? four[l].v : four[l].k, *e = v ? four[l].v_scale : four[l].k_scale;
@@ -1897,6 +1905,11 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   if (!q || !out) return fail(ctx, ALORA_EINVAL, "q / out is NULL");
   const size_t esz = dtype == ALORA_BF16 ? 2 : 4;
   if ((uintptr_t)q % esz || (uintptr_t)out % esz) return fail(ctx, ALORA_EINVAL, "q / out is not aligned to its elements");
+  {
+    const char *qa = (const char *)q, *oa = (const char *)out;
+    const size_t n = (size_t)pl.T * n_q_heads * head_dim * esz;
+    if (qa < oa + n && oa < qa + n) return fail(ctx, ALORA_EINVAL, "q and out overlap");
+  }
   if ((int64_t)pl.T * n_q_heads > (1 << 30)) return fail(ctx, ALORA_EINVAL, "%d rows of %d heads are more than one call takes", pl.T, n_q_heads);
   if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
   if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "alora_qcache_attend stages its work list from the host: not under graph capture");
@@ -2020,6 +2033,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   }
   // Caches of 4 bits: the projection appends to a pool of the call's rows alone, in their order, from which they are stored.
   if (qc) {
+    if ((int64_t)pl.T * L.n_q_heads > (1 << 30)) return fail(ctx, ALORA_EINVAL, "%d rows of %d heads are more than one call takes", pl.T, L.n_q_heads);
     if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "calls on caches of 4 bits stage their work lists from the host: not under graph capture");
     run_pl = pl;
     for (SeqMeta &m : run_pl.seqs) { m.pool_off = (int64_t)m.row_start - m.P; m.prefix_off = 0; m.prefix_len = 0; }
@@ -2284,7 +2298,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     alora_kv_cache fresh{};
     fresh.k = ctx->ws + probe.bytes; fresh.v = ctx->ws + probe.bytes + new_bytes; fresh.pool_tokens = pl.T;
     project_rows<T>(ctx, &layers[l], L, &fresh, cur, ppl, seqs_dev, w, l == 0, 0, s);
-    const bool wide = L.head_dim % QBLOCK == 0 && ((uintptr_t)qc[l].k | (uintptr_t)qc[l].v) % 4 == 0;
+    const bool wide = L.head_dim % 8 == 0 && ((uintptr_t)qc[l].k | (uintptr_t)qc[l].v) % 4 == 0;
     store.planes = (const RowPlane *)(slot->dev + q_at + qseq_bytes + qattn_bytes + range_bytes) + 2 * l;
     {
       ProfScope p(ctx, K_ROWS, s);

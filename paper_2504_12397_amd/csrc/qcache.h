@@ -43,17 +43,17 @@ void launch_rows_copy(const RowsArgs &a, const RowsFew &few, hipStream_t s);
 // covers, all of them before it -- have been read.
 struct RowStep { int64_t src, dst; int32_t rows, dep0, dep1, pad_; };
 struct RowsOrderedArgs {
-  const RowStep *steps;
+  const RowStep *steps;          // both nullptr: in `few`, steps first
   const RowPlane *planes;
-  int n_steps, n_planes;
+  int n_steps, n_planes, planes_at;
   uint32_t *ticket;              // [n_planes], ROWS_TICKET_STRIDE apart (a line of memory each: one counter for all was 290 us of 19000 workgroups); 0 before and after a call
   uint32_t *read;                // [n_steps, n_planes]: `epoch` once the piece has been read
   uint32_t epoch;                // another one for every call on these flags
 };
 constexpr int ROWS_TICKET_STRIDE = 32, ROWS_ORDERED_PLANES = 1024;
 constexpr int ROWS_ORDERED_UNITS = 256 * 8;      // most units that a piece of any plane has
-void launch_rows_copy_ordered(const RowsOrderedArgs &a, hipStream_t s);
-// T rows of n_kv heads of head_dim <-> rows of 4 bits; wide: head_dim is a multiple of 32, rows begin at multiples of 16 bytes, codes of 4
+void launch_rows_copy_ordered(const RowsOrderedArgs &a, const RowsFew &few, hipStream_t s);
+// T rows of n_kv heads of head_dim <-> rows of 4 bits; wide: head_dim is a multiple of 8, rows begin at multiples of 16 bytes, codes of 4
 template <typename T> void launch_rows_store(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);
 template <typename T> void launch_rows_load(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);
 

@@ -137,7 +137,8 @@ def table(ab, q, off=(0, 50), cap=(50, 50), length=(10, 20), poff=None, plen=Non
     (dict(cu=[0, 10, 30]), "ALORA_EHIP"), (dict(off=[-1, 50]), "ALORA_ECAPACITY"), (dict(off=[0, 51]), "ALORA_ECAPACITY"), (dict(length=[51, 20]), "ALORA_ECAPACITY"),
     (dict(poff=[0, 0], plen=[0, 15], length=[10, 20]), "ALORA_EHIP"), (dict(poff=[0, 0], plen=[0, 15], cu=[0, 1, 7]), "ALORA_EINVAL"),
     (dict(poff=[0, 90], plen=[0, 15]), "ALORA_ECAPACITY"), (dict(poff=[0, 0], plen=[-1, 0]), "ALORA_EINVAL"), (dict(poff=[0, 0], plen=[0, 21]), "ALORA_EINVAL"),
-    (dict(off=[0, 0]), "ALORA_EHIP"), (dict(q=None), "ALORA_EINVAL"), (dict(out=None), "ALORA_EINVAL"), (dict(q=P + 1), "ALORA_EINVAL")])
+    (dict(off=[0, 0]), "ALORA_EHIP"), (dict(q=None), "ALORA_EINVAL"), (dict(out=None), "ALORA_EINVAL"), (dict(q=P + 1), "ALORA_EINVAL"),
+    (dict(out=P), "ALORA_EINVAL"), (dict(out=P + 2 * 3 * 256 - 16), "ALORA_EINVAL"), (dict(out=P + 2 * 3 * 256), "ALORA_EHIP")])
 def test_attend(ab, v, over, want):
     o = dict(dtype=1, n_q=4, h=64, B=2, cu=[0, 1, 3], q=P, out=2 * P)
     o.update({k: x for k, x in over.items() if k in o})
@@ -154,7 +155,7 @@ def test_attend_without_its_arrays(ab, v):
     q = four(ab)
     cu = np.array([0, 1], np.int32).ctypes.data_as(C.POINTER(C.c_int32))
     def call(q, cu=cu):
-        return status(ab, ab._lib.alora_qcache_attend(v, 1, 4, 2, 64, q, P, cu, 1, P, None))
+        return status(ab, ab._lib.alora_qcache_attend(v, 1, 4, 2, 64, q, P, cu, 1, 2 * P, None))
     assert call(C.byref(q)) == "ALORA_EINVAL"                # no table
     keep = table(ab, q)
     assert call(C.byref(q)) == "ALORA_EHIP" and call(None) == "ALORA_EINVAL" and call(C.byref(q), None) == "ALORA_EINVAL"

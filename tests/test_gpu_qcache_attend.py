@@ -336,6 +336,20 @@ def test_prefill_and_decode(ab, ctx, shape, decode):
     check_layers(ab, ctx, case, four, full, out, decode)
 
 
+def test_plain_kernels(ab):
+    """The option that forces the kernels for any shape, on the layers' path."""
+    c = ab.Context(0)
+    try:
+        c.set_option("kernels", 1)
+        case = H.make_case(SMALL_BF16, [90, 0, 33], [3, 40, 1], [90, 0, 40], [0, 1, -1], seed=23, prefix="random")
+        full = H.gpu_cache(case)
+        four = q_copy(ab, c, full)
+        out = ab.alora_qcache_prefill(c, H.gpu_layer(case, SMALL_BF16), four, case.x_packed.cuda().contiguous(), case.cu, case.k, case.adapter)
+        check_layers(ab, c, case, four, full, out, False)
+    finally:
+        c.close()
+
+
 @pytest.mark.parametrize("decode", [False, True], ids=["prefill", "decode"])
 def test_adapters_on_shared_contexts(ab, ctx, decode):
     C, group, own = [150, 70], [0, 1, 0, -1, 0], [3, 0, 0, 9, 20]
