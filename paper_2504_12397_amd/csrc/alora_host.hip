@@ -1777,11 +1777,28 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
     // while even ranges of 32 keys a wave leave half of the chip idle, more waves share a head's keys
     while (c.hw > 1 && items_of(c.hw, 32 * (waves / (c.hw * c.cw))) * 2 <= slots) c.hw /= 2;
     c.kr = waves / (c.hw * c.cw);
+    // The range of keys: the shortest that one round of workgroups takes.
     int64_t r = std::max<int64_t>((longest + cap - 1) / cap, 128 * c.kr);
     if (ctx->opt_splits > 0) {
       r = std::max<int64_t>(1, (longest + ctx->opt_splits - 1) / ctx->opt_splits);
-    } else {
+    } else if (items_of(c.hw, longest) <= slots) {
       for (int i = 0; i < 64 && r < longest && items_of(c.hw, r) > slots; ++i) r += std::max<int64_t>(32, r / 16);
+    } else {
+      // More units than compute units: whole ones would leave a part of the chip idle at the end (300 sequences on 4000 keys 327 us, cut in parts 279 us).  The
+      // cut that takes least, in keys of one workgroup (1/20 us): QATTN_ITEM_KEYS for a workgroup's start and end, half a range that is uneven at the end,
+      // records written and read at 4.5 TB/s and the launch that joins them.
+      constexpr double QATTN_ITEM_KEYS = 170;
+      int64_t keys = 0;
+      for (const Unit &u : units[k])
+        keys += (int64_t)u.len * (((int64_t)u.n_rows * G + 16 * c.nc * c.cw - 1) / (16 * c.nc * c.cw)) * ((L.n_kv_heads + c.hw - 1) / c.hw);
+      const int64_t most = std::min<int64_t>(cap, std::max<int64_t>(1, longest / (128 * c.kr)));
+      double best = 0;
+      for (int64_t parts = 1; parts <= most; parts += std::max<int64_t>(1, parts / 8)) {
+        const int64_t len = (longest + parts - 1) / parts;
+        double cost = std::max(len + QATTN_ITEM_KEYS, (keys + QATTN_ITEM_KEYS * items_of(c.hw, len)) / slots + 0.5 * len);
+        if (parts > 1) cost += 140 + 20 * (double)pl.T * L.n_q_heads * parts * (L.head_dim + 2) * 8 / 4.5e6;
+        if (parts == 1 || cost < best) { best = cost; r = len; }
+      }
     }
     // (one row on 131072 keys: 256 records a head are merged in 9 us; half as many, with two waves on every head's keys, 46.9 -> 43.5 us, a quarter 45.5)
     if (ctx->opt_splits == 0 && c.kr == 1 && c.hw == 8 && longest > 128 * r) { c.hw = 4; c.kr = 2; r *= 2; }

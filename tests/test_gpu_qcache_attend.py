@@ -207,6 +207,18 @@ def test_long_sequences(ab, ctx, h, n_q, n_kv):
     b.check(ab.alora_qcache_attend(ctx, b.cache, b.q, b.cu, n_q))
 
 
+@pytest.mark.parametrize("dtype,h", [("bf16", 64), ("f32", 80)])
+def test_more_sequences_than_compute_units(ab, ctx, dtype, h):
+    """300 steps on the rows of three sequences: keys are cut in parts though there is a workgroup for every compute unit without."""
+    b = Batch(ab, dtype, 8, 8, h, [2100, 1999, 2050], [1, 1, 1], seed=17)
+    pick = [i % 3 for i in range(300)]
+    lens = [b.own[p] for p in pick]
+    cache = ab.QCache.from_tensors(b.cache.k, b.cache.v, b.cache.k_scale, b.cache.v_scale, [b.off[p] for p in pick], lens, lens)
+    out = ab.alora_qcache_attend(ctx, cache, b.q[pick], list(range(301)), 8)
+    assert torch.equal(out, out[:3][pick])
+    b.check(out[:3])
+
+
 def test_positions_far_into_a_pool(ab, ctx):
     """A sequence whose rows lie past byte 2^32 of the codes, read from there."""
     b = Batch(ab, "bf16", 16, 16, 256, [70], [3], seed=13)
