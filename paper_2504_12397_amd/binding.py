@@ -238,6 +238,7 @@ class KVCache(_Pool):
 
     def _refresh(self):
         self.desc = KVCacheDesc(_ptr(self.k), _ptr(self.v), self.pool_tokens, *self._tables())
+        self.kind = (int(self.k.shape[1]), self.head_dim, self.k.dtype)
 
     def rows(self, b: int, lo: int, hi: int):
         o = int(self.seq_offset[b])
@@ -270,7 +271,7 @@ class QCache(_Pool):
                      seq_capacity=None, seq_len=None, prefix_offset=None, prefix_len=None) -> "QCache":
         """A cache over tensors that exist; the table only where a call needs it."""
         h = 2 * int(k.shape[-1])
-        assert k.shape == v.shape and k_scale.shape == v_scale.shape == (*k.shape[:2], (h + Q_BLOCK - 1) // Q_BLOCK), "codes and exponents of one cache"
+        assert k.dim() == 3 and k.shape == v.shape and k_scale.shape == v_scale.shape == (*k.shape[:2], (h + Q_BLOCK - 1) // Q_BLOCK), "codes and exponents of one cache"
         assert all(t.dtype == torch.uint8 for t in (k, v, k_scale, v_scale)), "codes and exponents are uint8"
         self = cls.__new__(cls)
         self.head_dim = h
@@ -279,6 +280,7 @@ class QCache(_Pool):
 
     def _refresh(self):
         self.desc = QCacheDesc(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), self.pool_tokens, *self._tables())
+        self.kind = (int(self.k.shape[1]), self.head_dim, self.k.dtype)
 
 
 class Context:
@@ -449,14 +451,14 @@ def _address(a: np.ndarray) -> int:
 def _move(name: str, ctx: Context, dst, src, ranges, stream, typed=None):
     """The four calls that move rows: caches are one, or a list of them, one per layer; typed: the side whose type the call is told."""
     d, s = ([dst] if isinstance(dst, _Pool) else dst), ([src] if isinstance(src, _Pool) else src)
-    if len(d) != len(s):
+    if len(d) != len(s) or len(d) == 0:
         raise ValueError(f"{len(d)} destination and {len(s)} source layers")
-    shapes = [(int(c.k.shape[1]), c.head_dim) for c in (d[0], s[0])]
-    if shapes[0] != shapes[1] or (typed is None and d[0].k.dtype != s[0].k.dtype):
-        raise ValueError(f"caches of different shapes or types: {shapes[0]} {d[0].k.dtype} and {shapes[1]} {s[0].k.dtype}")
+    to, of = d[0].kind, s[0].kind
+    if any([c.kind != to for c in d]) or any([c.kind != of for c in s]) or to[:2] != of[:2] or (typed is None and to != of):
+        raise ValueError(f"caches of different shapes or types: {[c.kind for c in d]} and {[c.kind for c in s]}")
     r = np.ascontiguousarray(np.asarray(ranges, dtype=np.int64).reshape(-1, 3))
-    kind = () if name == "alora_qcache_copy" else (_DTYPES[(d if typed == "dst" else s)[0].k.dtype],)
-    ctx._check(getattr(_lib, name)(ctx._h, *kind, *shapes[0], b"".join([bytes(c.desc) for c in d]), b"".join([bytes(c.desc) for c in s]), len(d),
+    kind = () if name == "alora_qcache_copy" else (_DTYPES[(to if typed == "dst" else of)[2]],)
+    ctx._check(getattr(_lib, name)(ctx._h, *kind, *to[:2], b"".join([bytes(c.desc) for c in d]), b"".join([bytes(c.desc) for c in s]), len(d),
                                    _address(r), len(r), _stream_ptr(stream)))
 
 
@@ -488,8 +490,10 @@ def alora_qcache_attend(ctx: Context, cache: QCache, q: torch.Tensor, cu_seqlens
     h = cache.head_dim
     if out is None:
         out = torch.empty_like(q)
-    if q.shape != (int(cu[-1]), n_q_heads * h) or out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError(f"q {tuple(q.shape)} and out {tuple(out.shape)} have to be [{int(cu[-1])}, {n_q_heads * h}] of one type")
+    if q.dtype not in _DTYPES or q.shape != (int(cu[-1]), n_q_heads * h) or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError(f"q {tuple(q.shape)} and out {tuple(out.shape)} have to be [{int(cu[-1])}, {n_q_heads * h}], fp32 or bf16")
+    if cache.seq_len is None or len(cu) - 1 > len(cache.seq_len):
+        raise ValueError(f"{len(cu) - 1} sequences for a cache of {0 if cache.seq_len is None else len(cache.seq_len)}")
     ctx._check(_lib.alora_qcache_attend(ctx._h, _DTYPES[q.dtype], n_q_heads, int(cache.k.shape[1]), h, C.byref(cache.desc), _ptr(q), _address(cu),
                                         len(cu) - 1, _ptr(out), _stream_ptr(stream)))
     return out
@@ -499,6 +503,13 @@ def _q_call(name, ctx, layers, caches, x, cu, k_per_seq, adapter_per_seq, out, w
     """The four calls on QCaches that run layers; cu = None: one row per sequence; width: columns of the output."""
     kk, ad = _i32(k_per_seq), _i32(adapter_per_seq)
     stack = "stack" in name
+    T = len(kk) if cu is None else int(cu[-1])
+    if len(layers) != len(caches) or any([c.kind[:2] != (l.desc.n_kv_heads, l.desc.head_dim) for l, c in zip(layers, caches)]):
+        raise ValueError(f"{len(layers)} layers and {len(caches)} caches, which have to be of the layers' heads")
+    if any([len(c.seq_len) < len(kk) for c in caches]) or len(ad) != len(kk) or (cu is not None and len(cu) != len(kk) + 1):
+        raise ValueError(f"{len(kk)} sequences, {len(ad)} adapters and caches of {[len(c.seq_len) for c in caches]}")
+    if x.shape != (T, layers[0].d) or x.dtype != layers[0].dtype or (out is not None and (out.shape != (T, width) or out.dtype != x.dtype)):
+        raise ValueError(f"x {tuple(x.shape)} has to be [{T}, {layers[0].d}] and out [{T}, {width}], both of the layers' type")
     if out is None:
         out = torch.empty((x.shape[0], width), dtype=layers[0].dtype, device=layers[0].device)
     p = C.POINTER(C.c_int32)

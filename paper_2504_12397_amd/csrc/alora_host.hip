@@ -2139,7 +2139,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     n_splits = pp.n_own + pp.n_sh;
   }
   QAttnPlan qp;
-  bool q_half = false;      // (caches of 4 bits: queries travel as fp16, as elsewhere, or as fp32)
+  bool q_half = false;      // (caches of 4 bits: queries travel as fp16, as elsewhere, or as fp32: to the plain kernels and those of fp32 layers)
   if (qc) {
     bool q_mfma = true, q_lds = true;
     for (int l = 0; l < n_layers; ++l) {
@@ -2147,8 +2147,6 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
       q_lds = q_lds && qattn_lds_supported(L, qc[l]);
     }
     q_half = q_mfma && layers[0].dtype == ALORA_BF16;
-    // (the plain kernels take bf16 layers' queries as fp32)
-    if (layers[0].dtype == ALORA_BF16 && !q_half) q_mfma = false;
     qp = plan_qattn(ctx, pl, L, q_half ? Q_F16 : Q_F32, q_mfma, q_lds);
     n_splits = qp.n_parts;
   }

@@ -207,6 +207,40 @@ def test_binding_refuses_what_does_not_fit(ab):
             ab.alora_qcache_attend(c, q, torch.zeros((3, 160)), [0, 2], 2, stream=FakeStream())
         with pytest.raises(ab.AloraError):
             ab.alora_qcache_copy(c, q, q, [(0, 20, 1)], stream=FakeStream())
+        # layers of another shape or type than the first, none at all
+        other = ab.QCache([4, 3], 1, 80, "cpu", guard_rows=1)
+        for d, s in (([q, other], [q, q]), ([q, q], [q, other]), ([], [])):
+            with pytest.raises(ValueError):
+                ab.alora_qcache_copy(c, d, s, [(0, 5, 1)], stream=FakeStream())
+        with pytest.raises(ValueError):
+            ab.alora_cache_copy(c, [k, k], [k, ab.KVCache([4], 2, 64, torch.float32, "cpu")], [(0, 2, 1)], stream=FakeStream())
+        # more sequences than the table has, queries of another type, rows that are not side by side
+        for n, dtype in ((3, torch.float32), (2, torch.float16)):
+            with pytest.raises(ValueError):
+                ab.alora_qcache_attend(c, q, torch.zeros((n, 160), dtype=dtype), list(range(n + 1)), 2, stream=FakeStream())
+        with pytest.raises(AssertionError):
+            ab.KVCache.from_tensors(torch.zeros(4, 2, 128)[..., :64], torch.zeros(4, 2, 128)[..., :64])
+    finally:
+        c.close()
+
+
+def test_binding_refuses_layers_and_rows_that_do_not_fit(ab):
+    layer = ab.Layer({"W_qkv": torch.zeros(4 * 64, 64)}, 2, 1, 64)
+    q = ab.QCache([4, 3], 1, 64, "cpu")
+    c = ab.Context(-1)
+
+    def call(cache=q, x=torch.zeros(2, 64), k=(0, 0), a=(-1, -1), out=None):
+        ab.alora_qcache_decode(c, layer, cache, x, k, a, attn_out=out, stream=FakeStream())
+    try:
+        for bad in (dict(cache=ab.QCache([4, 3], 2, 64, "cpu")), dict(cache=ab.QCache([4, 3], 1, 32, "cpu")), dict(cache=ab.QCache([4], 1, 64, "cpu")),
+                    dict(x=torch.zeros(1, 64)), dict(x=torch.zeros(2, 32)), dict(x=torch.zeros(2, 64, dtype=torch.bfloat16)), dict(a=(-1,)),
+                    dict(out=torch.zeros(2, 64)), dict(out=torch.zeros(2, 128, dtype=torch.bfloat16))):
+            with pytest.raises(ValueError):
+                call(**bad)
+        with pytest.raises(ValueError):
+            ab.alora_qcache_prefill(c, layer, q, torch.zeros(2, 64), [0, 2], (0, 0), (-1, -1), stream=FakeStream())
+        with pytest.raises(ab.AloraError, match="validation-only"):
+            call()
     finally:
         c.close()
 
