@@ -14,7 +14,7 @@
 // bits would add half of what the rounding of a bf16 result does), three for fp32.  Units of many columns, where the products count and not memory, take one operand
 // of fp16 (11 bits) with values of fp16, as long as that holds them exactly: a workgroup looks at the smallest exponent that it met and at whether its sums
 // are numbers, and says so where fp16 was too narrow; a second launch does those items, and no others, with operands of bf16.  128 rows of 32 heads on 32896 keys
-// 139 -> 120 us, the second launch (4 us) included.
+// 139 -> 117 us, the second launch (4 us) included.
 // The reference exponent of a column moves only when a score exceeds it by 2^8 more than it did: almost no step rescales the sums.  It begins 8 above the largest score
 // so far, so that probabilities are 1 at most (values may be as large as fp32 holds); in fp16 7 below it, for the sake of that type's small numbers: 2^15 at most.
 #pragma once
@@ -583,10 +583,13 @@ __global__ __launch_bounds__(512, OCC) void qattn_lds_kernel(QAttnArgs a) {
   const int v_at = R::ROWS + kg * hb + j * Tile::VB;      // slot of row 16 u + 4 kg + n: 16 u + 4 n + kg
   const int vs_at = 2 * R::ROWS + 256 + 16 * kg + e_in + Tile::CPL * j / QBLOCK;
   int slot = 0;
+  // HALF: products and conversions count, not memory.  No wave waits for another, and of the two on a SIMD one goes first, so that its products run beside the
+  // other's conversions (in step and alike: 300 rows each of 4 sequences on 3000 keys 154 us, so 148; 2500 rows 124, so 121).
+  if (HALF && wave >= 4) __builtin_amdgcn_s_setprio(2);
   for (int i = 0; i < w.steps; ++i) {
     // The heads of a token share lines of memory: waves that drift apart fetch them twice (64 x 16449 keys: 1.29 GB instead of 1.15, 248 us; so 206).
     // Every wave of the workgroup comes by here as often as the others.
-    __builtin_amdgcn_s_barrier();
+    if (!HALF) __builtin_amdgcn_s_barrier();
     const int k0 = w.kbeg + 32 * i;
     if (k0 >= w.kend) continue;
     wait_vm<(DEPTH - 1) * R::PER_STEP>();
