@@ -1905,12 +1905,12 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   // the checks of the other calls, on the lengths before the rows of the queries
   std::vector<int32_t> before(B), zero(B, 0), none(B, -1);
   for (int b = 0; b < B; ++b) {
-    const int S = cu[b + 1] - cu[b], plen = cache->prefix_len ? cache->prefix_len[b] : 0;
+    const int64_t S = (int64_t)cu[b + 1] - cu[b], plen = cache->prefix_len ? cache->prefix_len[b] : 0;
     if (S < 0) return fail(ctx, ALORA_EINVAL, "cu_seqlens decreases at sequence %d", b);
     if (cache->seq_len[b] < 0) return fail(ctx, ALORA_EINVAL, "seq_len[%d] = %d is negative", b, cache->seq_len[b]);
-    if ((int64_t)S > (int64_t)cache->seq_len[b] - plen && S > 0)
-      return fail(ctx, ALORA_EINVAL, "sequence %d: %d queries, but only %lld rows of its own behind its prefix", b, S, (long long)cache->seq_len[b] - plen);
-    before[b] = cache->seq_len[b] - S;
+    if (S > cache->seq_len[b] - plen && S > 0)
+      return fail(ctx, ALORA_EINVAL, "sequence %d: %lld queries, but only %lld rows of its own behind its prefix", b, (long long)S, (long long)(cache->seq_len[b] - plen));
+    before[b] = (int32_t)(cache->seq_len[b] - S);
   }
   alora_kv_cache table = table_of(*cache);
   table.seq_len = before.data();

@@ -132,7 +132,7 @@ def table(ab, q, off=(0, 50), cap=(50, 50), length=(10, 20), poff=None, plen=Non
 
 @pytest.mark.parametrize("over,want", [
     (dict(), "ALORA_EHIP"), (dict(cu=[0, 0, 0]), "ALORA_OK"), (dict(dtype=9), "ALORA_EDTYPE"), (dict(n_q=5), "ALORA_ESHAPE"), (dict(n_q=0), "ALORA_ESHAPE"),
-    (dict(h=7), "ALORA_ESHAPE"), (dict(B=0), "ALORA_EINVAL"), (dict(cu=[1, 2, 3]), "ALORA_EINVAL"), (dict(cu=[0, 2, 1]), "ALORA_EINVAL"),
+    (dict(h=7), "ALORA_ESHAPE"), (dict(B=0), "ALORA_EINVAL"), (dict(cu=[1, 2, 3]), "ALORA_EINVAL"), (dict(cu=[0, 2, 1]), "ALORA_EINVAL"), (dict(cu=[2 ** 31 - 1, -2 ** 31, 3]), "ALORA_EINVAL"),
     (dict(cu=[0, 11, 12]), "ALORA_EINVAL"), (dict(length=[-1, 20]), "ALORA_EINVAL"), (dict(length=[0, 20]), "ALORA_EINVAL"),
     (dict(cu=[0, 10, 30]), "ALORA_EHIP"), (dict(off=[-1, 50]), "ALORA_ECAPACITY"), (dict(off=[0, 51]), "ALORA_ECAPACITY"), (dict(length=[51, 20]), "ALORA_ECAPACITY"),
     (dict(poff=[0, 0], plen=[0, 15], length=[10, 20]), "ALORA_EHIP"), (dict(poff=[0, 0], plen=[0, 15], cu=[0, 1, 7]), "ALORA_EINVAL"),
