@@ -10,10 +10,10 @@
 //   * V: lane (j, kg) has CPL = HT / 16 channels from CPL j on of those 8 keys; after conversion a byte permute of two keys' words puts
 //     one channel of two keys side by side, which is the transposition: product c is channel CPL i + c of lane row i.
 // No LDS and no barrier but where several waves share a head's keys (KR > 1): they join at the end, in pairs.
-// Queries of bf16 are one operand, exactly; fp16 two (high and low bits as bf16), fp32 three.  Probabilities are two operands (16 bits; one of 8
+// Queries of bf16 are one operand, exactly; fp16 two (high and low bits as bf16; one beside keys of fp16, below), fp32 three.  Probabilities are two operands (16 bits; one of 8
 // bits would add half of what the rounding of a bf16 result does), three for fp32.  Units of many columns, where the products count and not memory, take one operand
 // of fp16 (11 bits) with values of fp16, as long as that holds them exactly: a workgroup looks at the smallest exponent that it met and at whether its sums
-// are numbers, and says so where fp16 was too narrow; a second launch does those items, and no others, with operands of bf16.  128 rows of 32 heads on 32896 keys
+// are numbers (queries of fp16 take keys of fp16 likewise: both ends of their exponents count), and says so where fp16 was too narrow; a second launch does those items, and no others, with operands of bf16.  128 rows of 32 heads on 32896 keys
 // 139 -> 117 us, the second launch (4 us) included.
 // The reference exponent of a column moves only when a score exceeds it by 2^8 more than it did: almost no step rescales the sums.  It begins 8 above the largest score
 // so far, so that probabilities are 1 at most (values may be as large as fp32 holds); in fp16 7 below it, for the sake of that type's small numbers: 2^15 at most.
@@ -30,7 +30,7 @@ typedef float qa_f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 qa_f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 qa_f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr uint32_t QA_F16_FIRST = 114;      // the first exponent byte whose smallest value, 0.5 * 2^(E - 127), is a normal number of fp16
+constexpr uint32_t QA_F16_FIRST = 114, QA_F16_LAST = 140;      // the exponent bytes whose smallest value, 0.5 * 2^(E - 127), and largest, 6 * 2^(E - 127), are normal numbers of fp16
 
 // byte b of w: two codes, as a pair of bf16
 __device__ __forceinline__ uint32_t qa_pair(uint32_t w, float scale, int b) {
@@ -130,17 +130,19 @@ template <int HT> struct QaTile {
 };
 
 // The columns of a wave: queries, running sums, and what is done with 32 keys.
-// HALF: probabilities and values as fp16.
+// HALF: probabilities and values as fp16; K16: keys too, beside queries of fp16 (one operand instead of two).
 template <int HT, int NQ, int NP, int NC, bool HALF, typename TQ, typename T> struct QaColumns {
   typedef QaTile<HT> Tile;
   static constexpr float ABOVE = HALF ? -7.f : 8.f, LAZY = HALF ? 15.f : 0.f;      // log2 units: where a new reference lies, how far a score may exceed it
   static constexpr int KS = Tile::KS, CPL = Tile::CPL, VW = Tile::VW, KSC = Tile::KSC;
+  static constexpr bool K16 = HALF && NQ == 1 && __is_same(TQ, _Float16);
   uint32_t qf[NC][NQ][KS][4];
   int lim[NC];                            // last key that the column sees
   qa_f32x4 o[NC][CPL];                    // o[c][v] of lane (j, kg): channel CPL * (4 kg + v) + c of column j
   float m_ref[NC], neg_m[NC], l[NC];      // reference exponent (log2), its negative or 0 where there is none, this lane's part of the sum
   uint32_t nan_blocks[NC];                // blocks of 32 channels in which the column has met a value that is not a number
   uint32_t e_min;                         // HALF: the smallest exponent of a value so far
+  uint32_t k_far;                         // K16: how far above QA_F16_FIRST a key's exponent was (below: wrapped)
   int j, kg;
   float c_scale;
 
@@ -190,6 +192,7 @@ template <int HT, int NQ, int NP, int NC, bool HALF, typename TQ, typename T> st
       nan_blocks[nc] = 0;
     }
     e_min = 255;
+    k_far = 0;
   }
 
   // Some value was too small for fp16, or too large (the sums are infinite or no numbers; or they would be so anyway).
@@ -201,7 +204,7 @@ template <int HT, int NQ, int NP, int NC, bool HALF, typename TQ, typename T> st
       for (int c = 0; c < CPL; ++c)
 #pragma unroll
         for (int v = 0; v < 4; ++v) z += o[nc][c][v] - o[nc][c][v];
-    return e_min < QA_F16_FIRST || !(z == 0.f);
+    return e_min < QA_F16_FIRST || k_far > QA_F16_LAST - QA_F16_FIRST || !(z == 0.f);
   }
 
   // 32 keys from k0 on.  k_used() is called once t.k has been read, need_v() before t.v is, v_used() after.
@@ -216,13 +219,15 @@ template <int HT, int NQ, int NP, int NC, bool HALF, typename TQ, typename T> st
       for (int s = 0; s < KS; ++s) {
         const float e = qa_scale(t.ks[u][KSC == 2 ? s / 4 : 0]);
         const uint32_t c = t.k[u][s];
-        const qa_u32x4 kf = {qa_pair(c, e, 0), qa_pair(c, e, 1), qa_pair(c, e, 2), qa_pair(c, e, 3)};
+        const qa_u32x4 kf = K16 ? qa_u32x4{qa_pair16(c, e, 0), qa_pair16(c, e, 1), qa_pair16(c, e, 2), qa_pair16(c, e, 3)}
+                                : qa_u32x4{qa_pair(c, e, 0), qa_pair(c, e, 1), qa_pair(c, e, 2), qa_pair(c, e, 3)};
 #pragma unroll
         for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
           for (int p = 0; p < NQ; ++p) {
             const qa_u32x4 qv = {qf[nc][p][s][0], qf[nc][p][s][1], qf[nc][p][s][2], qf[nc][p][s][3]};
-            sc[nc][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(qa_bf16x8, kf), __builtin_bit_cast(qa_bf16x8, qv), sc[nc][u], 0, 0, 0);
+            if constexpr (K16) sc[nc][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(qa_f16x8, kf), __builtin_bit_cast(qa_f16x8, qv), sc[nc][u], 0, 0, 0);
+            else sc[nc][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(qa_bf16x8, kf), __builtin_bit_cast(qa_bf16x8, qv), sc[nc][u], 0, 0, 0);
           }
       }
     }
@@ -233,7 +238,8 @@ template <int HT, int NQ, int NP, int NC, bool HALF, typename TQ, typename T> st
       asm volatile("" : "+v"(first));      // (the comparisons stay here: made ahead of the branch they cost every step 17 instructions and as many pairs of registers)
       bool bad = false;
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
+        if (K16 && first - 4 * kg + 16 * u + j >= w.kend) t.ks[u][0] = 127;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const int key = first + 16 * u + v;
@@ -243,6 +249,7 @@ template <int HT, int NQ, int NP, int NC, bool HALF, typename TQ, typename T> st
           for (int nc = 0; nc < NC; ++nc)
             if (key >= w.kend || key > lim[nc]) sc[nc][u][v] = -INFINITY;
         }
+      }
       if (__any(bad)) {
         // 0 times NaN would reach the columns that do not see the key: its values count as 0, and the columns that do see it remember the block
         const int nb = q_blocks(a.head_dim);
@@ -266,6 +273,7 @@ template <int HT, int NQ, int NP, int NC, bool HALF, typename TQ, typename T> st
           }
       }
     }
+    if constexpr (K16) k_far = max(k_far, max(t.ks[0][0] - QA_F16_FIRST, t.ks[1][0] - QA_F16_FIRST));
     constexpr int PP = HALF ? 1 : NP;
     uint32_t pf[NC][PP][4];
 #pragma unroll

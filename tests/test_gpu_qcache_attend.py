@@ -362,6 +362,27 @@ def test_plain_kernels(ab):
         c.close()
 
 
+@pytest.mark.parametrize("k_pow,q_pow", [(0, 0), (15, -14), (-16, 13)], ids=["as_usual", "over_fp16", "under_fp16"])
+def test_keys_around_what_fp16_holds(ab, ctx, k_pow, q_pow):
+    """Many rows of a sequence multiply in fp16 where it holds every key: here half of the channels' keys are far over it, or below its normal numbers, and the
+    queries' the other way, so that scores are of the usual size."""
+    shape = SMALL_BF16
+    case = H.make_case(shape, [200, 70], [40, 33], [999, 999], [-1, -1], seed=24, prefix="random")
+    channels = torch.arange(shape.head_dim) % 64 < 32       # (whole blocks, and both halves of a rotation)
+    scale = torch.ones(shape.n_qkv, 1)
+    scale[:shape.n_q][channels.repeat(shape.n_q_heads)] = 2.0 ** q_pow
+    scale[shape.n_q:shape.n_q + shape.n_kv][channels.repeat(shape.n_kv_heads)] = 2.0 ** k_pow
+    W = case.tensors["W_qkv"]
+    case.tensors["W_qkv"] = (W.float() * scale).to(W.dtype)
+    case.layer = H.oracle_layer(case.tensors, shape)
+    for K in case.cache_K:
+        K[:, channels.repeat(shape.n_kv_heads).numpy()] *= 2.0 ** k_pow
+    full = H.gpu_cache(case)
+    four = q_copy(ab, ctx, full)
+    out = ab.alora_qcache_prefill(ctx, H.gpu_layer(case, shape), four, case.x_packed.cuda().contiguous(), case.cu, case.k, case.adapter)
+    check_layers(ab, ctx, case, four, full, out, False)
+
+
 @pytest.mark.parametrize("decode", [False, True], ids=["prefill", "decode"])
 def test_adapters_on_shared_contexts(ab, ctx, decode):
     C, group, own = [150, 70], [0, 1, 0, -1, 0], [3, 0, 0, 9, 20]
