@@ -185,12 +185,24 @@ class _Pool:
         self.seq_offset, self.seq_capacity = _table(seq_offset, np.int64), _table(seq_capacity, np.int32)
         self.seq_len = _table(seq_len, np.int32)
         self.prefix_offset, self.prefix_len = _table(prefix_offset, np.int64), _table(prefix_len, np.int32)
+        own, shared = (self.seq_offset, self.seq_capacity, self.seq_len), (self.prefix_offset, self.prefix_len)
+        if len({len(t) for t in own + (shared if shared[1] is not None else ()) if t is not None}) > 1 or (shared[1] is not None and shared[0] is None):
+            raise ValueError(f"tables of {[None if t is None else len(t) for t in own + shared]} sequences")
         self._refresh()
         return self
 
+    def _holds(self, n: int) -> bool:
+        """Every table that a call of n sequences reads is there and as long as that: the library reads them on the host, as far as the call says."""
+        need = (self.seq_offset, self.seq_capacity, self.seq_len) + (() if self.prefix_len is None else (self.prefix_offset, self.prefix_len))
+        return all([t is not None and len(t) >= n for t in need])
+
     def _tables(self):
         def of(a, t):
-            return None if a is None else a.ctypes.data_as(C.POINTER(t))
+            if a is None:
+                return None
+            if a.dtype != t or not a.flags.c_contiguous:
+                raise ValueError(f"a table of {a.dtype} (contiguous: {a.flags.c_contiguous}) where the library reads {t.__name__} side by side")
+            return a.ctypes.data_as(C.POINTER(t))
         shared = self.prefix_len is not None
         return (of(self.seq_offset, C.c_int64), of(self.seq_capacity, C.c_int32), of(self.seq_len, C.c_int32),
                 of(self.prefix_offset, C.c_int64) if shared else None, of(self.prefix_len, C.c_int32))
@@ -498,8 +510,8 @@ def alora_qcache_attend(ctx: Context, cache: QCache, q: torch.Tensor, cu_seqlens
         out = torch.empty_like(q)
     if q.dtype not in _DTYPES or q.shape != (int(cu[-1]), n_q_heads * h) or out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError(f"q {tuple(q.shape)} and out {tuple(out.shape)} have to be [{int(cu[-1])}, {n_q_heads * h}], fp32 or bf16")
-    if cache.seq_len is None or len(cu) - 1 > len(cache.seq_len):
-        raise ValueError(f"{len(cu) - 1} sequences for a cache of {0 if cache.seq_len is None else len(cache.seq_len)}")
+    if not cache._holds(len(cu) - 1):
+        raise ValueError(f"{len(cu) - 1} sequences are more than the tables of the cache hold")
     ctx._check(_lib.alora_qcache_attend(ctx._h, _DTYPES[q.dtype], n_q_heads, int(cache.k.shape[1]), h, C.byref(cache.desc), _ptr(q), _address(cu),
                                         len(cu) - 1, _ptr(out), _stream_ptr(stream)))
     return out
@@ -512,8 +524,9 @@ def _q_call(name, ctx, layers, caches, x, cu, k_per_seq, adapter_per_seq, out, w
     T = len(kk) if cu is None else int(cu[-1])
     if len(layers) != len(caches) or any([c.kind[:2] != (l.desc.n_kv_heads, l.desc.head_dim) for l, c in zip(layers, caches)]):
         raise ValueError(f"{len(layers)} layers and {len(caches)} caches, which have to be of the layers' heads")
-    if any([len(c.seq_len) < len(kk) for c in caches]) or len(ad) != len(kk) or (cu is not None and len(cu) != len(kk) + 1):
-        raise ValueError(f"{len(kk)} sequences, {len(ad)} adapters and caches of {[len(c.seq_len) for c in caches]}")
+    lengths = [0 if c.seq_len is None else len(c.seq_len) for c in caches]
+    if any([n != lengths[0] for n in lengths]) or not caches[0]._holds(len(kk)) or len(ad) != len(kk) or (cu is not None and len(cu) != len(kk) + 1):
+        raise ValueError(f"{len(kk)} sequences, {len(ad)} adapters and caches of {lengths}, which have to be as many in every layer and in every table")
     if x.shape != (T, layers[0].d) or x.dtype != layers[0].dtype or (out is not None and (out.shape != (T, width) or out.dtype != x.dtype)):
         raise ValueError(f"x {tuple(x.shape)} has to be [{T}, {layers[0].d}] and out [{T}, {width}], both of the layers' type")
     if out is None:

@@ -1,0 +1,91 @@
+"""CPU-side checks of what the calls on rows of a cache refuse beyond single bad arguments: tables of different lengths, arrays that lie over each other, sizes that no
+launch or address takes, and the order in which errors are found.  Nothing is launched (validation-only context, device -1)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from tests.test_abi_qcache import FakeStream, GOOD, P, four, full, ranges, status, table
+
+
+@pytest.fixture(scope="module")
+def ab():
+    from paper_2504_12397_amd import binding
+    return binding
+
+
+@pytest.fixture()
+def v(ab):
+    h = C.c_void_p()
+    assert ab._lib.alora_create(C.byref(h), -1) == ab.ALORA_OK
+    yield h
+    ab._lib.alora_destroy(h)
+
+
+# ---- tables of the binding's caches ---------------------------------------------------------------------------------
+def tensors(ab, rows=20):
+    t = lambda *s: torch.zeros(s, dtype=torch.uint8)  # noqa: E731
+    return t(rows, 1, 32), t(rows, 1, 32), t(rows, 1, 2), t(rows, 1, 2)
+
+
+@pytest.mark.parametrize("tables", [dict(seq_offset=[0]), dict(seq_capacity=[5, 5, 5]), dict(seq_len=[1]), dict(prefix_offset=[0], prefix_len=[0, 0]),
+                                    dict(prefix_offset=[0, 0], prefix_len=[0]), dict(prefix_len=[0, 0])])
+def test_tables_of_different_lengths(ab, tables):
+    good = dict(seq_offset=[0, 10], seq_capacity=[5, 5], seq_len=[1, 2])
+    kv = torch.zeros((20, 1, 64))
+    ab.QCache.from_tensors(*tensors(ab), **good)
+    ab.KVCache.from_tensors(kv, kv.clone(), **good)
+    with pytest.raises(ValueError):
+        ab.QCache.from_tensors(*tensors(ab), **dict(good, **tables))
+    with pytest.raises(ValueError):
+        ab.KVCache.from_tensors(kv, kv.clone(), **dict(good, **tables))
+
+
+@pytest.mark.parametrize("change", [dict(seq_offset=np.zeros(1, np.int64)), dict(seq_capacity=np.zeros(1, np.int32)), dict(prefix_len=np.zeros(1, np.int32)),
+                                    dict(prefix_offset=np.zeros(1, np.int64)), dict(seq_offset=None), dict(seq_len=None), dict(prefix_offset=None)])
+def test_calls_on_tables_that_are_too_short(ab, change):
+    """Tables set by hand: a call names more sequences than one of them has."""
+    layer = ab.Layer({"W_qkv": torch.zeros(4 * 64, 64)}, 2, 1, 64)
+    q = ab.QCache.from_tensors(*tensors(ab), seq_offset=[0, 10], seq_capacity=[5, 5], seq_len=[1, 2], prefix_offset=[0, 0], prefix_len=[0, 0])
+    c = ab.Context(-1)
+    try:
+        def calls():
+            yield lambda: ab.alora_qcache_attend(c, q, torch.zeros(2, 128), [0, 1, 2], 2, stream=FakeStream())
+            yield lambda: ab.alora_qcache_decode(c, layer, q, torch.zeros(2, 64), [0, 0], [-1, -1], stream=FakeStream())
+            yield lambda: ab.alora_qcache_prefill(c, layer, q, torch.zeros(2, 64), [0, 1, 2], [0, 0], [-1, -1], stream=FakeStream())
+        for call in calls():
+            with pytest.raises(ab.AloraError, match="validation-only"):
+                call()
+        for name, value in change.items():
+            setattr(q, name, value)
+        for call in calls():
+            with pytest.raises(ValueError):
+                call()
+    finally:
+        c.close()
+
+
+def test_stacks_on_tables_of_different_lengths(ab):
+    """The lengths of the first layer's cache are copied to the others after the call: they have to be as many."""
+    layer = ab.Layer({"W_qkv": torch.zeros(4 * 64, 64)}, 2, 1, 64)
+    c = ab.Context(-1)
+    table = dict(seq_offset=[0, 10], seq_capacity=[5, 5], seq_len=[1, 2])
+    try:
+        for other in (dict(seq_offset=[0, 10, 15], seq_capacity=[5, 5, 5], seq_len=[1, 2, 0]), dict()):
+            caches = [ab.QCache.from_tensors(*tensors(ab), **t) for t in (table, other)]
+            with pytest.raises(ValueError):
+                ab.alora_qcache_stack_decode(c, [layer, layer], caches, torch.zeros(2, 64), [0, 0], [-1, -1], stream=FakeStream())
+    finally:
+        c.close()
+
+
+def test_tables_of_other_types(ab):
+    q = ab.QCache.from_tensors(*tensors(ab), seq_offset=[0, 10], seq_capacity=[5, 5], seq_len=[1, 2])
+    for name, bad in (("seq_offset", np.zeros(2, np.int32)), ("seq_len", np.zeros(2, np.int64)), ("seq_capacity", np.zeros(4, np.int32)[::2])):
+        was = getattr(q, name)
+        setattr(q, name, bad)
+        with pytest.raises(ValueError):
+            q._refresh()
+        setattr(q, name, was)
+        q._refresh()
