@@ -1993,6 +1993,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   Plan pl;
   pl.L = L;
   if (n_steps < 1) return fail(ctx, ALORA_EINVAL, "n_steps = %d must be at least 1", n_steps);
+  if (qc && (st = check_qcaches(ctx, qc, n_layers)) != ALORA_OK) return st;
   st = check_batch(ctx, &layers[0], &caches[0], cu, kps, aps, B, n_steps, &pl);
   if (st != ALORA_OK) return st;
   if (pl.T > 0 && (!x || !out)) return fail(ctx, ALORA_EINVAL, "x / out is NULL");
@@ -2725,11 +2726,9 @@ alora_status alora_qcache_attend(alora_ctx *ctx, int32_t dtype, int32_t n_q_head
 static alora_status run_q(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, alora_qcache *caches, const void *x, const int32_t *cu,
                           const int32_t *kps, const int32_t *aps, int B, void *out, void *stream, bool stack, bool decode) {
   return guarded(ctx, [&] {
+    if (decode && B < 1) return fail(ctx, ALORA_EINVAL, "B = %d must be at least 1", B);
     if (n_layers < 1) return fail(ctx, ALORA_EINVAL, "n_layers = %d must be at least 1", n_layers);
     if (!layers || !caches) return fail(ctx, ALORA_EINVAL, "layers / caches is NULL");
-    if (decode && B < 1) return fail(ctx, ALORA_EINVAL, "B = %d must be at least 1", B);
-    alora_status st = check_qcaches(ctx, caches, n_layers);
-    if (st != ALORA_OK) return st;
     std::vector<int32_t> one;
     if (decode)
       for (int b = 0; b <= B; ++b) one.push_back(b);

@@ -89,3 +89,37 @@ def test_tables_of_other_types(ab):
             q._refresh()
         setattr(q, name, was)
         q._refresh()
+
+
+# ---- the order in which errors are found ------------------------------------------------------------------------------
+@pytest.mark.parametrize("desc,tables,want", [(dict(heads=3), dict(), "ALORA_ESHAPE"), (dict(dtype=7), dict(), "ALORA_EDTYPE"), (dict(d=0), dict(length=(50, 20)), "ALORA_ESHAPE"),
+                                              (dict(), dict(length=(50, 20)), "ALORA_EINVAL")])
+def test_errors_of_layers_come_first(ab, v, desc, tables, want):
+    """A call with two mistakes names the one that the call on other caches names: the layer before the cache's arrays, these before the sequences."""
+    desc, p = layer_desc(ab, **desc), full(ab, k=None)
+    cu, zero, none = np.array([0, 1, 2], np.int32), np.zeros(2, np.int32), np.full(2, -1, np.int32)
+    keep = [table(ab, p, **tables)]
+    st = ab._lib.alora_prefill(v, C.byref(desc), C.byref(p), P, arg(cu), arg(zero), arg(none), 2, P, None)
+    assert status(ab, st) == want
+    for name in ("k", "k_scale"):
+        q = four(ab)
+        setattr(q, name, None)
+        keep.append(table(ab, q, **tables))
+        assert layer_calls(ab, v, desc, q, cu) == [want] * 2, name
+        for fn in (lambda *a: ab._lib.alora_qcache_decode(v, C.byref(desc), *a), lambda *a: ab._lib.alora_qcache_stack_decode(v, C.byref(desc), 1, *a)):
+            assert status(ab, fn(C.byref(q), P, arg(zero), arg(none), 2, P, None)) == want, name
+
+
+def layer_desc(ab, heads=4, kv=2, h=64, dtype=1, d=64):
+    return ab.LayerDesc(d, heads, kv, h, 0, 0, dtype, 128, P, None, None, None, None, None, P, 1e-5, 1e4, P, P, P, P, P)
+
+
+def arg(a):
+    return a.ctypes.data_as(C.POINTER(C.c_int32))
+
+
+def layer_calls(ab, v, desc, cache, cu, x=P, out=P):
+    B = len(cu) - 1
+    cu, zero, none = np.array(cu, np.int32), np.zeros(B, np.int32), np.full(B, -1, np.int32)
+    return [status(ab, ab._lib.alora_qcache_prefill(v, C.byref(desc), C.byref(cache), x, arg(cu), arg(zero), arg(none), B, out, None)),
+            status(ab, ab._lib.alora_qcache_stack_prefill(v, C.byref(desc), 1, C.byref(cache), x, arg(cu), arg(zero), arg(none), B, out, None))]
