@@ -325,16 +325,16 @@ alora_status check_batch(alora_ctx *ctx, const alora_layer_desc *ly, const alora
     if (kps[b] < 0) return fail(ctx, ALORA_EINVAL, "k_per_seq[%d] = %d is negative", b, kps[b]);
     if (aps[b] < -1 || aps[b] >= ly->n_adapters)
       return fail(ctx, ALORA_EADAPTER, "adapter_per_seq[%d] = %d outside [-1, %d)", b, aps[b], ly->n_adapters);
-    if (cap < 0 || off < 0 || off + cap > cache->pool_tokens)
-      return fail(ctx, ALORA_ECAPACITY, "sequence %d: rows [%lld, %lld) lie outside the pool of %lld tokens", b,
-                  (long long)off, (long long)(off + cap), (long long)cache->pool_tokens);
+    if (cap < 0 || off < 0 || cap > cache->pool_tokens || off > cache->pool_tokens - cap)
+      return fail(ctx, ALORA_ECAPACITY, "sequence %d: %d rows from %lld on lie outside the pool of %lld tokens", b, cap,
+                  (long long)off, (long long)cache->pool_tokens);
     const int plen = cache->prefix_len ? cache->prefix_len[b] : 0;
     const int64_t poff = plen > 0 ? cache->prefix_offset[b] : 0;
     if (plen < 0 || plen > P)
       return fail(ctx, ALORA_EINVAL, "sequence %d: prefix_len = %d outside [0, seq_len = %d]", b, plen, P);
-    if (plen > 0 && (poff < 0 || poff + plen > cache->pool_tokens))
-      return fail(ctx, ALORA_ECAPACITY, "sequence %d: shared prefix rows [%lld, %lld) lie outside the pool of %lld tokens",
-                  b, (long long)poff, (long long)(poff + plen), (long long)cache->pool_tokens);
+    if (plen > 0 && (poff < 0 || plen > cache->pool_tokens || poff > cache->pool_tokens - plen))
+      return fail(ctx, ALORA_ECAPACITY, "sequence %d: %d shared prefix rows from %lld on lie outside the pool of %lld tokens",
+                  b, plen, (long long)poff, (long long)cache->pool_tokens);
     const int64_t grown = (int64_t)P + (int64_t)S * n_steps;      // cached length after the call
     if (grown - plen > cap)
       return fail(ctx, ALORA_ECAPACITY, "sequence %d: %d cached + %lld new tokens exceed its capacity %d", b, P - plen,
@@ -1632,20 +1632,26 @@ alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int
   return ALORA_OK;
 }
 
+// Arrays whose bytes no address reaches are refused here, so that sums and products of rows and bytes stay in 64 bits everywhere else.
+alora_status check_pool(alora_ctx *ctx, int64_t tokens, int64_t row_bytes) {
+  if (tokens > (1ll << 62) / row_bytes) return fail(ctx, ALORA_ECAPACITY, "pool_tokens = %lld rows of %lld bytes are more than memory", (long long)tokens, (long long)row_bytes);
+  return ALORA_OK;
+}
+int64_t row_bytes_of(int dtype, int n_kv_heads, int head_dim) { return (int64_t)n_kv_heads * head_dim * (dtype == ALORA_BF16 ? 2 : 4); }
 // The arrays of a cache of 4 bits are there, and of the same size in all layers.
-alora_status check_qcaches(alora_ctx *ctx, const alora_qcache *c, int n_layers) {
+alora_status check_qcaches(alora_ctx *ctx, const alora_qcache *c, int n_layers, int n_kv_heads, int head_dim) {
   for (int l = 0; l < n_layers; ++l) {
     if (!c[l].k || !c[l].v || !c[l].k_scale || !c[l].v_scale) return fail(ctx, ALORA_EINVAL, "layer %d: k, v, k_scale or v_scale is NULL", l);
     if (c[l].pool_tokens != c[0].pool_tokens) return fail(ctx, ALORA_ECAPACITY, "layer %d: pool size differs from layer 0", l);
   }
-  return ALORA_OK;
+  return check_pool(ctx, c[0].pool_tokens, (int64_t)n_kv_heads * std::max(head_dim / 2, q_blocks(head_dim)));
 }
-alora_status check_caches(alora_ctx *ctx, const alora_kv_cache *c, int n_layers) {
+alora_status check_caches(alora_ctx *ctx, const alora_kv_cache *c, int n_layers, int64_t row_bytes) {
   for (int l = 0; l < n_layers; ++l) {
     if (!c[l].k || !c[l].v) return fail(ctx, ALORA_EINVAL, "layer %d: k or v is NULL", l);
     if (c[l].pool_tokens != c[0].pool_tokens) return fail(ctx, ALORA_ECAPACITY, "layer %d: pool size differs from layer 0", l);
   }
-  return ALORA_OK;
+  return check_pool(ctx, c[0].pool_tokens, row_bytes);
 }
 
 // Storing (store) and loading: rows of the storage type in `full`, rows of 4 bits in `four`.
@@ -1653,8 +1659,8 @@ alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_di
                           int n_layers, const alora_row_range *ranges, int n_ranges, hipStream_t s) {
   if (dtype != ALORA_F32 && dtype != ALORA_BF16) return fail(ctx, ALORA_EDTYPE, "dtype %d is neither ALORA_F32 nor ALORA_BF16", dtype);
   alora_status st = check_row_shape(ctx, n_kv_heads, head_dim, n_layers, four, full);
-  if (st == ALORA_OK) st = check_qcaches(ctx, four, n_layers);
-  if (st == ALORA_OK) st = check_caches(ctx, full, n_layers);
+  if (st == ALORA_OK) st = check_qcaches(ctx, four, n_layers, n_kv_heads, head_dim);
+  if (st == ALORA_OK) st = check_caches(ctx, full, n_layers, row_bytes_of(dtype, n_kv_heads, head_dim));
   RowJob job;
   if (st == ALORA_OK)
     st = store ? check_ranges(ctx, ranges, n_ranges, full->pool_tokens, four->pool_tokens, false, &job)
@@ -1897,7 +1903,7 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
   if (st != ALORA_OK) return st;
   if (n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % n_kv_heads != 0)
     return fail(ctx, ALORA_ESHAPE, "n_q_heads = %d must be a positive multiple of n_kv_heads = %d", n_q_heads, n_kv_heads);
-  st = check_qcaches(ctx, cache, 1);
+  st = check_qcaches(ctx, cache, 1, n_kv_heads, head_dim);
   if (st != ALORA_OK) return st;
   if (B < 1) return fail(ctx, ALORA_EINVAL, "B = %d must be at least 1", B);
   if (!cu) return fail(ctx, ALORA_EINVAL, "cu_seqlens is NULL");
@@ -1993,7 +1999,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   Plan pl;
   pl.L = L;
   if (n_steps < 1) return fail(ctx, ALORA_EINVAL, "n_steps = %d must be at least 1", n_steps);
-  if (qc && (st = check_qcaches(ctx, qc, n_layers)) != ALORA_OK) return st;
+  if (qc && (st = check_qcaches(ctx, qc, n_layers, L.n_kv_heads, L.head_dim)) != ALORA_OK) return st;
   st = check_batch(ctx, &layers[0], &caches[0], cu, kps, aps, B, n_steps, &pl);
   if (st != ALORA_OK) return st;
   if (pl.T > 0 && (!x || !out)) return fail(ctx, ALORA_EINVAL, "x / out is NULL");
@@ -2675,10 +2681,10 @@ alora_status alora_cache_copy(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads,
   return guarded(ctx, [&] {
     if (dtype != ALORA_F32 && dtype != ALORA_BF16) return fail(ctx, ALORA_EDTYPE, "dtype %d is neither ALORA_F32 nor ALORA_BF16", dtype);
     alora_status st = check_row_shape(ctx, n_kv_heads, head_dim, n_layers, dst, src);
-    if (st == ALORA_OK) st = check_caches(ctx, dst, n_layers);
-    if (st == ALORA_OK) st = check_caches(ctx, src, n_layers);
+    const int64_t row = row_bytes_of(dtype, n_kv_heads, head_dim);
+    if (st == ALORA_OK) st = check_caches(ctx, dst, n_layers, row);
+    if (st == ALORA_OK) st = check_caches(ctx, src, n_layers, row);
     if (st != ALORA_OK) return st;
-    const int64_t row = (int64_t)n_kv_heads * head_dim * (dtype == ALORA_BF16 ? 2 : 4);
     std::vector<CopyArray> arrays;
     for (int l = 0; l < n_layers; ++l) {
       arrays.push_back(CopyArray{src[l].k, dst[l].k, row});
@@ -2692,8 +2698,8 @@ alora_status alora_qcache_copy(alora_ctx *ctx, int32_t n_kv_heads, int32_t head_
                                int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream) {
   return guarded(ctx, [&] {
     alora_status st = check_row_shape(ctx, n_kv_heads, head_dim, n_layers, dst, src);
-    if (st == ALORA_OK) st = check_qcaches(ctx, dst, n_layers);
-    if (st == ALORA_OK) st = check_qcaches(ctx, src, n_layers);
+    if (st == ALORA_OK) st = check_qcaches(ctx, dst, n_layers, n_kv_heads, head_dim);
+    if (st == ALORA_OK) st = check_qcaches(ctx, src, n_layers, n_kv_heads, head_dim);
     if (st != ALORA_OK) return st;
     const int64_t codes = (int64_t)n_kv_heads * (head_dim / 2), scales = (int64_t)n_kv_heads * q_blocks(head_dim);
     std::vector<CopyArray> arrays;

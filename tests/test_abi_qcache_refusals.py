@@ -123,3 +123,36 @@ def layer_calls(ab, v, desc, cache, cu, x=P, out=P):
     cu, zero, none = np.array(cu, np.int32), np.zeros(B, np.int32), np.full(B, -1, np.int32)
     return [status(ab, ab._lib.alora_qcache_prefill(v, C.byref(desc), C.byref(cache), x, arg(cu), arg(zero), arg(none), B, out, None)),
             status(ab, ab._lib.alora_qcache_stack_prefill(v, C.byref(desc), 1, C.byref(cache), x, arg(cu), arg(zero), arg(none), B, out, None))]
+
+
+# ---- sizes ----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("off,poff", [(2 ** 63 - 1, 0), (2 ** 63 - 20, 0), (50, 2 ** 63 - 1), (50, 2 ** 63 - 6)])
+def test_rows_whose_end_is_past_every_number(ab, v, off, poff):
+    """offset + capacity and offset + prefix are over 2^63: outside the pool, not at its front."""
+    q, k = four(ab), full(ab)
+    tables = dict(off=(0, off), cap=(50, 50), length=(10, 20), poff=(0, poff), plen=(0, 8))
+    keep = [table(ab, c, **tables) for c in (q, k)]
+    cu = np.array([0, 1, 2], np.int32)
+    assert status(ab, ab._lib.alora_qcache_attend(v, 1, 4, 2, 64, C.byref(q), P, arg(cu), 2, 2 * P, None)) == "ALORA_ECAPACITY"
+    desc = layer_desc(ab)
+    assert layer_calls(ab, v, desc, q, cu) == ["ALORA_ECAPACITY"] * 2
+    zero, none = np.zeros(2, np.int32), np.full(2, -1, np.int32)
+    st = ab._lib.alora_prefill(v, C.byref(desc), C.byref(k), P, arg(cu), arg(zero), arg(none), 2, P, None)
+    assert status(ab, st) == "ALORA_ECAPACITY" and keep
+
+
+@pytest.mark.parametrize("tokens", [2 ** 62, 2 ** 57, 2 ** 63 - 1])
+def test_pools_that_no_address_reaches(ab, v, tokens):
+    """pool_tokens times the bytes of a row is over 2^62."""
+    lib, r = ab._lib, ranges(ab, GOOD)
+    big, small, qbig, qsmall = full(ab, tokens=tokens), full(ab, 7 * P, 8 * P), four(ab, tokens=tokens), four(ab, 9 * P, 10 * P, 11 * P, 12 * P)
+    for st in (lib.alora_cache_copy(v, 1, 2, 64, C.byref(big), C.byref(small), 1, r, 1, None), lib.alora_cache_copy(v, 1, 2, 64, C.byref(small), C.byref(big), 1, r, 1, None),
+               lib.alora_qcache_copy(v, 2, 64, C.byref(qbig), C.byref(qsmall), 1, r, 1, None),
+               lib.alora_qcache_store(v, 1, 2, 64, C.byref(qbig), C.byref(small), 1, r, 1, None),
+               lib.alora_qcache_store(v, 1, 2, 64, C.byref(qsmall), C.byref(big), 1, r, 1, None),
+               lib.alora_qcache_load(v, 1, 2, 64, C.byref(big), C.byref(qsmall), 1, r, 1, None)):
+        assert status(ab, st) == "ALORA_ECAPACITY"
+    keep = table(ab, qbig)
+    cu = np.array([0, 1, 2], np.int32)
+    assert status(ab, lib.alora_qcache_attend(v, 1, 4, 2, 64, C.byref(qbig), P, arg(cu), 2, 2 * P, None)) == "ALORA_ECAPACITY"
+    assert layer_calls(ab, v, layer_desc(ab), qbig, cu) == ["ALORA_ECAPACITY"] * 2 and keep
