@@ -352,7 +352,7 @@ alora_status alora_cache_copy(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads,
 /* The same for rows of 4 bits: codes and exponents. */
 alora_status alora_qcache_copy(alora_ctx *ctx, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *dst, const alora_qcache *src,
                                int32_t n_layers, const alora_row_range *ranges, int32_t n_ranges, void *stream);
-/* Rows of the storage type into rows of 4 bits, and back.  Ranges as above; dst and src never share memory.  Calls of all four kinds whose ranges and
+/* Rows of the storage type into rows of 4 bits, and back.  Ranges as above; dst and src never share memory (ALORA_EINVAL where those of a layer do).  Calls of all four kinds whose ranges and
  * arrays travel as kernel arguments (24 bytes a range, 32 an array -- two a layer, four with 4 bits on both sides -- 3584 bytes in all) launch one kernel and
  * nothing else, unless rows move over each other: such a call may be captured into a HIP graph.  Under capture the others are refused (ALORA_EINVAL). */
 alora_status alora_qcache_store(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *dst,

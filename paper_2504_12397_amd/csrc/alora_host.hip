@@ -1473,6 +1473,9 @@ alora_status move_rows(alora_ctx *ctx, std::vector<RowRange> ranges, const std::
   return ALORA_OK;
 }
 
+bool share_memory(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes) {
+  return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
+}
 uint32_t copy_unit(const void *dst, const void *src, int64_t row_bytes) {
   const uintptr_t m = (uintptr_t)dst | (uintptr_t)src | (uintptr_t)row_bytes;
   return m % 16 == 0 ? 16 : m % 4 == 0 ? 4 : 1;
@@ -1577,8 +1580,7 @@ alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int
   for (const CopyArray &c : arrays) {
     if (!c.dst || !c.src) return fail(ctx, ALORA_EINVAL, "an array of a cache is NULL");
     if ((c.dst == c.src) != in_place) return fail(ctx, ALORA_EINVAL, "some arrays of dst and src are the same and some are not");
-    const char *d = (const char *)c.dst, *r = (const char *)c.src;
-    if (!in_place && d < r + src_tokens * c.row_bytes && r < d + dst_tokens * c.row_bytes)
+    if (!in_place && share_memory(c.dst, dst_tokens * c.row_bytes, c.src, src_tokens * c.row_bytes))
       return fail(ctx, ALORA_EINVAL, "dst and src overlap in memory and are not the same array");
     widest = std::max(widest, c.row_bytes);
   }
@@ -1670,6 +1672,12 @@ alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_di
   for (int l = 0; l < n_layers; ++l)
     for (const void *p : {full[l].k, full[l].v})
       if ((uintptr_t)p % esz) return fail(ctx, ALORA_EINVAL, "layer %d: k or v is not aligned to its elements", l);
+  const int64_t full_bytes = full->pool_tokens * row_bytes_of(dtype, n_kv_heads, head_dim), heads = four->pool_tokens * n_kv_heads;
+  for (int l = 0; l < n_layers; ++l)
+    for (const void *p : {full[l].k, full[l].v})
+      if (share_memory(p, full_bytes, four[l].k, heads * (head_dim / 2)) || share_memory(p, full_bytes, four[l].v, heads * (head_dim / 2)) ||
+          share_memory(p, full_bytes, four[l].k_scale, heads * q_blocks(head_dim)) || share_memory(p, full_bytes, four[l].v_scale, heads * q_blocks(head_dim)))
+        return fail(ctx, ALORA_EINVAL, "layer %d: rows of 4 bits and of the storage type overlap in memory", l);
   if (job.ranges.empty()) return ALORA_OK;
   if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
   HIP_TRY(ctx, hipSetDevice(ctx->device));

@@ -156,3 +156,24 @@ def test_pools_that_no_address_reaches(ab, v, tokens):
     cu = np.array([0, 1, 2], np.int32)
     assert status(ab, lib.alora_qcache_attend(v, 1, 4, 2, 64, C.byref(qbig), P, arg(cu), 2, 2 * P, None)) == "ALORA_ECAPACITY"
     assert layer_calls(ab, v, layer_desc(ab), qbig, cu) == ["ALORA_ECAPACITY"] * 2 and keep
+
+
+# ---- arrays that lie over each other ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("name", ["k", "v", "k_scale", "v_scale"])
+@pytest.mark.parametrize("side", ["k", "v"])
+@pytest.mark.parametrize("call", ["qcache_store", "qcache_load"])
+def test_rows_and_their_codes_lie_apart(ab, v, call, side, name):
+    """The rows of the storage type and those of 4 bits share no memory: codes that begin inside the rows, that end in them, and that lie right behind and right before."""
+    lib, r, rows = ab._lib, ranges(ab, GOOD), 100
+    row = 2 * 64 * 2                              # bytes of a row, and of its codes or exponents
+    mine = 2 * 32 if "scale" not in name else 2 * 2
+    def run(at):
+        f, q = full(ab, 40 * P, 41 * P, rows), four(ab, tokens=rows)
+        setattr(q, name, getattr(f, side) + at)
+        fn = lib.alora_qcache_store if call == "qcache_store" else lib.alora_qcache_load
+        a, b = (q, f) if call == "qcache_store" else (f, q)
+        return status(ab, fn(v, 1, 2, 64, C.byref(a), C.byref(b), 1, r, 1, None))
+    for at in (0, 64, rows * row - 64, 64 - rows * mine):
+        assert run(at) == "ALORA_EINVAL", at
+    for at in (rows * row, -rows * mine):
+        assert run(at) == "ALORA_EHIP", at
