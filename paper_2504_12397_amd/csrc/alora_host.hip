@@ -1421,12 +1421,16 @@ alora_status check_ranges(alora_ctx *ctx, const alora_row_range *r, int n, int64
   return ALORA_OK;
 }
 
-// Cuts the ranges in pieces of chunk_rows rows; false: too many for a grid.
+// A launch has fewer than 2^32 threads along x.
+constexpr int64_t LAUNCH_THREADS = 1ll << 32;
+constexpr const char *TOO_MANY_PIECES = "the call moves more pieces of rows than a launch takes (2^24)";
+
+// Cuts the ranges in pieces of chunk_rows rows; false: too many for a launch.
 bool cut_ranges(std::vector<RowRange> &ranges, int chunk_rows, int64_t *n_chunks) {
   int64_t n = 0;
   for (RowRange &q : ranges) { q.first_chunk = (uint32_t)n; n += ((int64_t)q.n + chunk_rows - 1) / chunk_rows; }
   *n_chunks = n;
-  return n <= 0x7fffffff;
+  return n * 256 < LAUNCH_THREADS;
 }
 // Rows of a piece: 32 KB of the widest array.  (Smaller pieces of small calls are slower: 17 rows of 2 KB in 64 arrays 16.8 us in pieces of 4 KB, 15.4 of 16 KB, 11.5 so.)
 int chunk_rows_of(int64_t row_bytes) { return (int)std::max<int64_t>(1, std::min<int64_t>(4096, 32768 / std::max<int64_t>(row_bytes, 1))); }
@@ -1440,7 +1444,7 @@ alora_status move_rows(alora_ctx *ctx, std::vector<RowRange> ranges, const std::
   a.n_ranges = (int)ranges.size();
   a.n_planes = (int)planes.size();
   a.chunk_rows = chunk_rows;
-  if (!cut_ranges(ranges, chunk_rows, &a.n_chunks) || a.n_planes > 65535) return fail(ctx, ALORA_EINVAL, "the call moves more rows than a grid takes");
+  (void)cut_ranges(ranges, chunk_rows, &a.n_chunks);      // (not too many: checked with the arguments)
   const bool cap = is_capturing(s);
   MetaSlot *slot = nullptr;
   if (rows_are_few(ranges.size(), planes.size())) {
@@ -1509,7 +1513,7 @@ alora_status copy_rows_ordered(alora_ctx *ctx, const RowJob &job, const std::vec
       const int64_t n = std::min<int64_t>(chunk, q.n - at), off = down ? at : q.n - at - n;
       steps.push_back(RowStep{q.src + off, q.dst + off, (int32_t)n, 0, 0, 0});
     }
-  if ((int64_t)steps.size() * (int64_t)planes.size() > (1 << 24)) return ALORA_OK;
+  if ((int64_t)steps.size() * (int64_t)planes.size() * 256 >= LAUNCH_THREADS) return ALORA_OK;
   // the pieces whose sources a destination covers: by their sources' order, the smallest and the largest place of them
   std::vector<int> by_src(steps.size());
   for (size_t i = 0; i < steps.size(); ++i) by_src[i] = (int)i;
@@ -1589,9 +1593,11 @@ alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int
   alora_status st = check_ranges(ctx, ranges, n_ranges, src_tokens, dst_tokens, in_place, &job);
   if (st != ALORA_OK) return st;
   if (job.ranges.empty()) return ALORA_OK;
+  const int chunk = chunk_rows_of(widest);
+  int64_t n_chunks;
+  if (!cut_ranges(job.ranges, chunk, &n_chunks)) return fail(ctx, ALORA_EINVAL, "%s", TOO_MANY_PIECES);
   if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
   HIP_TRY(ctx, hipSetDevice(ctx->device));
-  const int chunk = chunk_rows_of(widest);
   auto copy = [&](const std::vector<RowRange> &r, const std::vector<RowPlane> &planes) {
     return move_rows(ctx, r, planes, chunk, s, [&](const RowsArgs &a, const RowsFew &few) { launch_rows_copy(a, few, s); });
   };
@@ -1679,6 +1685,9 @@ alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_di
           share_memory(p, full_bytes, four[l].k_scale, heads * q_blocks(head_dim)) || share_memory(p, full_bytes, four[l].v_scale, heads * q_blocks(head_dim)))
         return fail(ctx, ALORA_EINVAL, "layer %d: rows of 4 bits and of the storage type overlap in memory", l);
   if (job.ranges.empty()) return ALORA_OK;
+  const int chunk = chunk_rows_of(row_bytes_of(dtype, n_kv_heads, head_dim));
+  int64_t n_chunks;
+  if (!cut_ranges(job.ranges, chunk, &n_chunks)) return fail(ctx, ALORA_EINVAL, "%s", TOO_MANY_PIECES);
   if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
   HIP_TRY(ctx, hipSetDevice(ctx->device));
   std::vector<RowPlane> planes;
@@ -1690,7 +1699,6 @@ alora_status convert_rows(alora_ctx *ctx, int dtype, int n_kv_heads, int head_di
       wide = wide && (uintptr_t)f % 16 == 0 && (uintptr_t)q % 4 == 0;
       planes.push_back(store ? RowPlane{f, q, e, 0, 0} : RowPlane{q, f, e, 0, 0});
     }
-  const int chunk = chunk_rows_of((int64_t)n_kv_heads * head_dim * (int64_t)esz);
   return move_rows(ctx, job.ranges, planes, chunk, s, [&](const RowsArgs &a, const RowsFew &few) {
     if (store && esz == 2) launch_rows_store<bf16>(a, few, n_kv_heads, head_dim, wide, s);
     else if (store) launch_rows_store<float>(a, few, n_kv_heads, head_dim, wide, s);
@@ -1708,6 +1716,7 @@ struct QAttnClass {
 };
 struct QAttnPlan {
   bool mfma = false, lds = false;
+  bool fits = true;                      // no launch of it has 2^32 threads; otherwise nothing below is filled in
   int n_parts = 1, first_shared = 0;
   std::vector<int32_t> row_seq;          // plain kernel: every row's sequence
   QAttnClass cls[2];
@@ -1726,6 +1735,7 @@ struct QAttnPlan {
     put(counts.data(), counts.size() * 4, up(counts.size() * 4));
   }
 };
+constexpr const char *TOO_MANY_ROWS = "%d rows of %d heads are more than one call takes";
 int qattn_ht(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 bool qattn_mfma_supported(const alora_ctx *ctx, const LayerDims &L, const alora_qcache &c, const void *q, const void *out) {
   return ctx->opt_kernels == 0 && L.head_dim % 8 == 0 && (((uintptr_t)c.k | (uintptr_t)c.v) & 3) == 0 && (((uintptr_t)q | (uintptr_t)out) & 15) == 0 &&
@@ -1741,7 +1751,10 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
   QAttnPlan q;
   q.mfma = mfma;
   q.lds = lds;
+  const bool wave_each = ((int64_t)pl.T * L.n_q_heads + 3) * 64 < LAUNCH_THREADS;      // a wave for every (row, head): the plain kernel, and the one that joins records
   if (!mfma) {
+    q.fits = wave_each;
+    if (!q.fits) return q;
     q.row_seq.resize(pl.T);
     for (int b = 0; b < pl.B; ++b)
       std::fill_n(q.row_seq.begin() + pl.seqs[b].row_start, pl.seqs[b].n_new, b);
@@ -1824,6 +1837,15 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
     for (const Unit &u : units[k]) (u.shared ? n_shared : n_own) = std::max(u.shared ? n_shared : n_own, (u.len + range[k] - 1) / range[k]);
   q.n_parts = n_own + n_shared;
   q.first_shared = n_own;
+  q.fits = q.n_parts == 1 || wave_each;
+  for (int k = 0; k < 2; ++k) {
+    int64_t n = 0;
+    const int wide = 16 * q.cls[k].nc * q.cls[k].cw;
+    for (const Unit &u : units[k])
+      n += ((u.len + (int64_t)range[k] - 1) / range[k]) * (((int64_t)u.n_rows * G + wide - 1) / wide) * ((L.n_kv_heads + q.cls[k].hw - 1) / q.cls[k].hw);
+    q.fits = q.fits && n * qattn_waves(ht) * 64 < LAUNCH_THREADS;
+  }
+  if (!q.fits) return q;
   if (q.n_parts > 1) q.counts.assign((size_t)2 * pl.T, 0);
   for (int k = 0; k < 2; ++k) {
     QAttnClass &c = q.cls[k];
@@ -1941,15 +1963,16 @@ alora_status attend_q(alora_ctx *ctx, int dtype, int n_q_heads, int n_kv_heads, 
     const size_t n = (size_t)pl.T * n_q_heads * head_dim * esz;
     if (qa < oa + n && oa < qa + n) return fail(ctx, ALORA_EINVAL, "q and out overlap");
   }
-  if ((int64_t)pl.T * n_q_heads > (1 << 30)) return fail(ctx, ALORA_EINVAL, "%d rows of %d heads are more than one call takes", pl.T, n_q_heads);
-  if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
-  if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "alora_qcache_attend stages its work list from the host: not under graph capture");
-  HIP_TRY(ctx, hipSetDevice(ctx->device));
+  if ((int64_t)pl.T * n_q_heads > (1 << 30)) return fail(ctx, ALORA_EINVAL, TOO_MANY_ROWS, pl.T, n_q_heads);
   LayerDims L{};
   L.n_q_heads = n_q_heads; L.n_kv_heads = n_kv_heads; L.head_dim = head_dim;
   L.n_q = n_q_heads * head_dim; L.n_kv = n_kv_heads * head_dim; L.n_qkv = L.n_q + 2 * L.n_kv;
   const QueryType qt = dtype == ALORA_BF16 ? Q_BF16 : Q_F32;
   const QAttnPlan qp = plan_qattn(ctx, pl, L, qt, qattn_mfma_supported(ctx, L, *cache, q, out), qattn_lds_supported(L, *cache));
+  if (!qp.fits) return fail(ctx, ALORA_EINVAL, TOO_MANY_ROWS, pl.T, n_q_heads);
+  if (ctx->device < 0) return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)");
+  if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "alora_qcache_attend stages its work list from the host: not under graph capture");
+  HIP_TRY(ctx, hipSetDevice(ctx->device));
   const size_t partial_bytes = qp.n_parts > 1 ? (attn_plain_partial_floats(L, pl.T, qp.n_parts) * sizeof(float) + 255) & ~(size_t)255 : 0;
   st = ensure_workspace(ctx, partial_bytes + qp.narrow_bytes());
   if (st != ALORA_OK) return st;
@@ -2016,7 +2039,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     return fail(ctx, ALORA_EINVAL, "alora_decode_static does not take shared prefixes (prefix_len must be NULL or all zero)");
   // (the size question of the static entry point is answered on a validation-only context too, by the same plan)
   const auto validation_only = [&] { return fail(ctx, ALORA_EHIP, "arguments are valid, but this is a validation-only context (device -1)"); };
-  if (ctx->device < 0 && !use_static) return validation_only();
+  if (ctx->device < 0 && !use_static && !qc) return validation_only();      // (caches of 4 bits: so is whether a launch takes the rows)
   if (ctx->device >= 0) HIP_TRY(ctx, hipSetDevice(ctx->device));
   hipStream_t s = (hipStream_t)stream;
   const size_t esz = layers[0].dtype == ALORA_BF16 ? 2 : 4;
@@ -2065,8 +2088,8 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
   }
   // Caches of 4 bits: the projection appends to a pool of the call's rows alone, in their order, from which they are stored.
   if (qc) {
-    if ((int64_t)pl.T * L.n_q_heads > (1 << 30)) return fail(ctx, ALORA_EINVAL, "%d rows of %d heads are more than one call takes", pl.T, L.n_q_heads);
-    if (is_capturing(s)) return fail(ctx, ALORA_EINVAL, "calls on caches of 4 bits stage their work lists from the host: not under graph capture");
+    if ((int64_t)pl.T * L.n_q_heads > (1 << 30)) return fail(ctx, ALORA_EINVAL, TOO_MANY_ROWS, pl.T, L.n_q_heads);
+    if (ctx->device >= 0 && is_capturing(s)) return fail(ctx, ALORA_EINVAL, "calls on caches of 4 bits stage their work lists from the host: not under graph capture");
     run_pl = pl;
     for (SeqMeta &m : run_pl.seqs) { m.pool_off = (int64_t)m.row_start - m.P; m.prefix_off = 0; m.prefix_len = 0; }
   }
@@ -2163,6 +2186,8 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     }
     q_half = q_mfma && layers[0].dtype == ALORA_BF16;
     qp = plan_qattn(ctx, pl, L, q_half ? Q_F16 : Q_F32, q_mfma, q_lds);
+    if (!qp.fits) return fail(ctx, ALORA_EINVAL, TOO_MANY_ROWS, pl.T, L.n_q_heads);
+    if (ctx->device < 0) return validation_only();
     n_splits = qp.n_parts;
   }
   const Plan &att_pl = run_prefill ? run_att : pl;      // the rows that attend together: sequence after sequence (the kernel finds where they lie)
@@ -2250,7 +2275,7 @@ alora_status run(alora_ctx *ctx, const alora_layer_desc *layers, int n_layers, a
     for (const SeqMeta &m : pl.seqs)
       if (m.n_new > 0) new_rows.push_back(RowRange{m.row_start, m.pool_off + m.P, (uint32_t)m.n_new, 0});
     store.chunk_rows = chunk_rows_of((int64_t)L.n_kv * (int64_t)esz);
-    if (!cut_ranges(new_rows, store.chunk_rows, &store.n_chunks)) return fail(ctx, ALORA_EINVAL, "the call stores more rows than a grid takes");
+    if (!cut_ranges(new_rows, store.chunk_rows, &store.n_chunks)) return fail(ctx, ALORA_EINVAL, "%s", TOO_MANY_PIECES);
     store.n_ranges = (int)new_rows.size();
     store.n_planes = 2;
     for (int l = 0; l < n_layers; ++l) {

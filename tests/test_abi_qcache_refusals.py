@@ -177,3 +177,47 @@ def test_rows_and_their_codes_lie_apart(ab, v, call, side, name):
         assert run(at) == "ALORA_EINVAL", at
     for at in (rows * row, -rows * mine):
         assert run(at) == "ALORA_EHIP", at
+
+
+# ---- what a launch takes ----------------------------------------------------------------------------------------------
+def many(ab, T, per=2 ** 20, prefix=0):
+    """A cache whose sequences have T rows in all, each all of its rows."""
+    B = (T + per - 1) // per
+    n = [min(per, T - b * per) for b in range(B)]
+    off = [prefix + b * per for b in range(B)]
+    q = four(ab, tokens=T + prefix)
+    keep = table(ab, q, off=off, cap=n, length=[m + prefix for m in n], poff=[0] * B if prefix else None, plen=[prefix] * B if prefix else None)
+    return q, keep, np.array([0] + list(np.cumsum(n)), np.int32)
+
+
+@pytest.mark.parametrize("T,heads,kv,h,prefix,want", [
+    (2 ** 22 - 1, 16, 16, 2, 0, "ALORA_EHIP"), (2 ** 22, 16, 16, 2, 0, "ALORA_EINVAL"), (2 ** 21, 64, 1, 34, 0, "ALORA_EINVAL"),      # a workgroup for each row and head
+    (2 ** 21, 64, 8, 128, 0, "ALORA_EHIP"),                                                                                           # many columns a workgroup
+    (2 ** 21, 64, 8, 128, 4, "ALORA_EINVAL"), (2 ** 21 - 1, 32, 8, 128, 4, "ALORA_EHIP")])                                            # two records a row and head are joined
+def test_attention_of_more_rows_than_a_launch_takes(ab, v, T, heads, kv, h, prefix, want):
+    q, keep, cu = many(ab, T, prefix=prefix)
+    far = 2 ** 44
+    assert status(ab, ab._lib.alora_qcache_attend(v, 1, heads, kv, h, C.byref(q), P, arg(cu), len(cu) - 1, far, None)) == want
+    q, keep, _ = many(ab, T, prefix=prefix)
+    for c in keep[2:3]:
+        c[:] = prefix                             # the layers' rows are new
+    desc = layer_desc(ab, heads=heads, kv=kv, h=h)
+    assert layer_calls(ab, v, desc, q, cu, out=far)[0] == want
+
+
+@pytest.mark.parametrize("call", ["cache_copy", "qcache_store"])
+def test_more_pieces_than_a_launch_takes(ab, v, call):
+    """2^24 ranges of a row each: a workgroup of 256 for every one."""
+    lib, n = ab._lib, 2 ** 24
+    r = np.zeros((n, 3), np.int64)
+    r[:, 0] = np.arange(n)
+    r[:, 1] = np.arange(n) + (n if "copy" in call else 0)
+    r[:, 2] = 1
+    tokens = 2 * n
+    a, b = full(ab, 2 ** 40, 2 ** 41, tokens), full(ab, 2 ** 42, 2 ** 43, tokens)
+    c = four(ab, 2 ** 44, 2 ** 45, 2 ** 46, 2 ** 47, tokens)
+    for m, want in ((n, "ALORA_EINVAL"), (n - 1, "ALORA_EHIP")):
+        p = r.ctypes.data
+        st = {"cache_copy": lambda: lib.alora_cache_copy(v, 1, 1, 2, C.byref(b), C.byref(a), 1, p, m, None),
+              "qcache_store": lambda: lib.alora_qcache_store(v, 1, 1, 2, C.byref(c), C.byref(a), 1, p, m, None)}[call]()
+        assert status(ab, st) == want
