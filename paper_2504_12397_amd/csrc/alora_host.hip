@@ -1374,6 +1374,11 @@ alora_status check_row_shape(alora_ctx *ctx, int n_kv_heads, int head_dim, int n
   return ALORA_OK;
 }
 
+// (they mostly come in order)
+template <typename T, typename Less> void sort_rows(std::vector<T> &v, Less less) {
+  if (!std::is_sorted(v.begin(), v.end(), less)) std::sort(v.begin(), v.end(), less);
+}
+
 // The ranges of a call, checked; those that leave rows where they are (in_place) and empty ones are dropped.
 struct RowJob {
   std::vector<RowRange> ranges;
@@ -1403,15 +1408,15 @@ alora_status check_ranges(alora_ctx *ctx, const alora_row_range *r, int n, int64
     job->ranges.push_back(q);
     job->rows += q.n;
   }
-  std::sort(by_dst.begin(), by_dst.end(), [](const RowRange &x, const RowRange &y) { return x.dst < y.dst; });
+  sort_rows(by_dst, [](const RowRange &x, const RowRange &y) { return x.dst < y.dst; });
   for (size_t i = 1; i < by_dst.size(); ++i)
     if (by_dst[i].dst < by_dst[i - 1].dst + by_dst[i - 1].n)
       return fail(ctx, ALORA_EINVAL, "destination rows [%lld, %lld) and [%lld, %lld) overlap", (long long)by_dst[i - 1].dst,
                   (long long)(by_dst[i - 1].dst + by_dst[i - 1].n), (long long)by_dst[i].dst, (long long)(by_dst[i].dst + by_dst[i].n));
   if (in_place && !job->ranges.empty()) {
     std::vector<RowRange> to(job->ranges), from(job->ranges);
-    std::sort(to.begin(), to.end(), [](const RowRange &x, const RowRange &y) { return x.dst < y.dst; });
-    std::sort(from.begin(), from.end(), [](const RowRange &x, const RowRange &y) { return x.src < y.src; });
+    sort_rows(to, [](const RowRange &x, const RowRange &y) { return x.dst < y.dst; });
+    sort_rows(from, [](const RowRange &x, const RowRange &y) { return x.src < y.src; });
     size_t j = 0;      // destinations are disjoint: in order of their ends as well
     for (const RowRange &f : from) {
       while (j < to.size() && to[j].dst + to[j].n <= f.src) ++j;
@@ -1506,28 +1511,46 @@ alora_status copy_rows_ordered(alora_ctx *ctx, const RowJob &job, const std::vec
   if (chunk < 1 || planes.size() > ROWS_ORDERED_PLANES) return ALORA_OK;
   chunk = std::min<int64_t>(chunk, chunk_rows_of(widest));
   std::vector<RowRange> r(job.ranges);
-  std::sort(r.begin(), r.end(), [&](const RowRange &x, const RowRange &y) { return down ? x.dst < y.dst : x.dst > y.dst; });
-  std::vector<RowStep> steps;
-  for (const RowRange &q : r)
-    for (int64_t at = 0; at < q.n; at += chunk) {
-      const int64_t n = std::min<int64_t>(chunk, q.n - at), off = down ? at : q.n - at - n;
-      steps.push_back(RowStep{q.src + off, q.dst + off, (int32_t)n, 0, 0, 0});
-    }
-  if ((int64_t)steps.size() * (int64_t)planes.size() * 256 >= LAUNCH_THREADS) return ALORA_OK;
-  // the pieces whose sources a destination covers: by their sources' order, the smallest and the largest place of them
-  std::vector<int> by_src(steps.size());
-  for (size_t i = 0; i < steps.size(); ++i) by_src[i] = (int)i;
-  std::sort(by_src.begin(), by_src.end(), [&](int x, int y) { return steps[x].src < steps[y].src; });
-  // (sources may overlap each other: a piece that begins before this destination ends at most `chunk` rows further on)
-  for (size_t i = 0; i < steps.size(); ++i) {
-    RowStep &st = steps[i];
-    auto lo = std::lower_bound(by_src.begin(), by_src.end(), st.dst - chunk, [&](int x, int64_t v) { return steps[x].src < v; });
-    int first = (int)steps.size(), last = -1;
-    for (; lo != by_src.end() && steps[*lo].src < st.dst + st.rows; ++lo)
-      if (steps[*lo].src + steps[*lo].rows > st.dst) { first = std::min(first, *lo); last = std::max(last, *lo); }
-    if (last >= 0) { st.dep0 = first; st.dep1 = std::min(last, (int)i) + 1; }      // (none comes after it)
+  sort_rows(r, [&](const RowRange &x, const RowRange &y) { return down ? x.dst < y.dst : x.dst > y.dst; });
+  // The ranges by their sources: the numbers of their first pieces in the order of destinations, and where the furthest of them and of those before them ends.
+  struct Source { int64_t at; int64_t n, first, reach; };
+  std::vector<Source> from;
+  int64_t n_pieces = 0;
+  for (const RowRange &q : r) { from.push_back(Source{q.src, q.n, n_pieces, 0}); n_pieces += ((int64_t)q.n + chunk - 1) / chunk; }
+  if (!down) std::reverse(from.begin(), from.end());
+  sort_rows(from, [](const Source &x, const Source &y) { return x.at < y.at; });
+  bool apart = true;
+  for (size_t i = 0; i < from.size(); ++i) {
+    from[i].reach = std::max(i ? from[i - 1].reach : 0, from[i].at + from[i].n);
+    apart = apart && (i == 0 || from[i - 1].reach <= from[i].at);
   }
-  const size_t tickets = (size_t)ROWS_ORDERED_PLANES * ROWS_TICKET_STRIDE, want = tickets + steps.size() * planes.size();
+  // every piece in the order of destinations: its range, its place there, its rows, and the first source that may reach behind its destination's begin
+  auto each_piece = [&](auto one) -> alora_status {
+    size_t j = down ? 0 : from.size();      // (destinations go one way)
+    for (const RowRange &q : r)
+      for (int64_t at = 0; at < q.n; at += chunk) {
+        const int64_t n = std::min<int64_t>(chunk, q.n - at), off = down ? at : q.n - at - n, dst = q.dst + off;
+        if (down) while (j < from.size() && from[j].reach <= dst) ++j;
+        else while (j > 0 && from[j - 1].reach > dst) --j;
+        const alora_status st = one(q, off, n, j);
+        if (st != ALORA_OK) return st;
+      }
+    return ALORA_OK;
+  };
+  // Where sources lie apart, destinations cover as many pieces as there are, or little more: the plan takes time in proportion to ranges and pieces (40000 ranges of a row 0.6 ms;
+  // a search from `chunk` rows before every destination 43).  Where they overlap (rows forked and covered in one call) it could take the square of that: such calls are staged.
+  if (!apart) {
+    int64_t left = 8 * (n_pieces + (int64_t)r.size()) + 1024;
+    const alora_status st = each_piece([&](const RowRange &q, int64_t off, int64_t n, size_t j) {
+      for (; j < from.size() && from[j].at < q.dst + off + n && left > 0; ++j) --left;
+      return left > 0 ? ALORA_OK : ALORA_EINVAL;
+    });
+    if (st != ALORA_OK) return ALORA_OK;
+  }
+  // So many pieces a launch: their table is staged, and a long move is several launches, one after the other (none of a later one's sources lies where an
+  // earlier one writes).  A million rows of 2 KB are two.
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(ROWS_ORDERED_STEPS, (LAUNCH_THREADS / 256 - 1) / (int64_t)planes.size()));
+  const size_t tickets = (size_t)ROWS_ORDERED_PLANES * ROWS_TICKET_STRIDE, want = tickets + (size_t)std::min(most, n_pieces) * planes.size();
   if (ctx->flags_cap < want) {
     HIP_TRY(ctx, hipDeviceSynchronize());
     if (ctx->flags) HIP_TRY(ctx, hipFree(ctx->flags));
@@ -1540,39 +1563,66 @@ alora_status copy_rows_ordered(alora_ctx *ctx, const RowJob &job, const std::vec
     ctx->flags_epoch = 0;
     HIP_TRY(ctx, hipDeviceSynchronize());
   }
-  if (++ctx->flags_epoch == 0) {      // (every 2^32 calls the flags begin anew)
-    HIP_TRY(ctx, hipDeviceSynchronize());
-    HIP_TRY(ctx, hipMemset(ctx->flags, 0, ctx->flags_cap * sizeof(uint32_t)));
-    HIP_TRY(ctx, hipDeviceSynchronize());
-    ctx->flags_epoch = 1;
-  }
-  RowsOrderedArgs a{nullptr, nullptr, (int)steps.size(), (int)planes.size(), 0, ctx->flags, ctx->flags + tickets, ctx->flags_epoch};
-  RowsFew few{};
-  const size_t sb = steps.size() * sizeof(RowStep), pb = (planes.size() * sizeof(RowPlane) + 15) & ~(size_t)15;
-  MetaSlot *slot = nullptr;
-  if (sb + pb <= ROWS_FEW_BYTES) {
-    a.planes_at = (int)sb;
-    memcpy(few.data, steps.data(), sb);
-    memcpy(few.data + sb, planes.data(), planes.size() * sizeof(RowPlane));
-  } else {
-    const alora_status got = acquire_slot(ctx, sb + pb, &slot);
-    if (got != ALORA_OK) return got;
-    memcpy(slot->host, steps.data(), sb);
-    memcpy(slot->host + sb, planes.data(), planes.size() * sizeof(RowPlane));
-    const int n16 = (int)((sb + pb) / 16);
-    hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
-    a.steps = (const RowStep *)slot->dev;
-    a.planes = (const RowPlane *)(slot->dev + sb);
-  }
-  {
-    ProfScope p(ctx, K_ROWS, s);
-    launch_rows_copy_ordered(a, few, s);
-  }
-  HIP_TRY(ctx, hipGetLastError());
-  if (slot) {
-    HIP_TRY(ctx, hipEventRecord(slot->ev, s));
-    slot->in_flight = true;
-  }
+  const size_t pb = (planes.size() * sizeof(RowPlane) + 15) & ~(size_t)15;
+  std::vector<RowStep> steps;
+  steps.reserve((size_t)std::min(most, n_pieces));
+  auto launch = [&]() -> alora_status {
+    if (++ctx->flags_epoch == 0) {      // (every 2^32 launches the flags begin anew)
+      HIP_TRY(ctx, hipDeviceSynchronize());
+      HIP_TRY(ctx, hipMemset(ctx->flags, 0, ctx->flags_cap * sizeof(uint32_t)));
+      HIP_TRY(ctx, hipDeviceSynchronize());
+      ctx->flags_epoch = 1;
+    }
+    RowsOrderedArgs a{nullptr, nullptr, (int)steps.size(), (int)planes.size(), 0, ctx->flags, ctx->flags + tickets, ctx->flags_epoch};
+    RowsFew few{};
+    const size_t sb = steps.size() * sizeof(RowStep);
+    MetaSlot *slot = nullptr;
+    if (sb + pb <= ROWS_FEW_BYTES) {
+      a.planes_at = (int)sb;
+      memcpy(few.data, steps.data(), sb);
+      memcpy(few.data + sb, planes.data(), planes.size() * sizeof(RowPlane));
+    } else {
+      const alora_status got = acquire_slot(ctx, sb + pb, &slot);
+      if (got != ALORA_OK) return got;
+      memcpy(slot->host, steps.data(), sb);
+      memcpy(slot->host + sb, planes.data(), planes.size() * sizeof(RowPlane));
+      const int n16 = (int)((sb + pb) / 16);
+      hipLaunchKernelGGL(stage_meta_kernel, dim3((n16 + 255) / 256), dim3(256), 0, s, (const uint4 *)slot->host, (uint4 *)slot->dev, n16);
+      a.steps = (const RowStep *)slot->dev;
+      a.planes = (const RowPlane *)(slot->dev + sb);
+    }
+    {
+      ProfScope p(ctx, K_ROWS, s);
+      launch_rows_copy_ordered(a, few, s);
+    }
+    HIP_TRY(ctx, hipGetLastError());
+    if (slot) {
+      HIP_TRY(ctx, hipEventRecord(slot->ev, s));
+      slot->in_flight = true;
+    }
+    steps.clear();
+    return ALORA_OK;
+  };
+  int64_t piece = 0, base = 0;                        // of all pieces; the launch's first
+  const alora_status st = each_piece([&](const RowRange &q, int64_t off, int64_t n, size_t j) {
+    const int64_t dst = q.dst + off;
+    int64_t first = n_pieces, last = -1;
+    for (; j < from.size() && from[j].at < dst + n; ++j) {      // its rows that this destination covers, and their pieces
+      const Source &f = from[j];
+      const int64_t lo = std::max(dst, f.at) - f.at, hi = std::min(dst + n, f.at + f.n) - 1 - f.at;
+      if (lo > hi) continue;
+      first = std::min(first, f.first + (down ? lo : f.n - 1 - hi) / chunk);
+      last = std::max(last, f.first + (down ? hi : f.n - 1 - lo) / chunk);
+    }
+    // (none comes after it, and those of earlier launches have been read)
+    const int64_t dep0 = std::max(first, base) - base, dep1 = std::min(last, piece) + 1 - base;
+    steps.push_back(RowStep{q.src + off, dst, (int32_t)n, (int32_t)(dep1 > dep0 ? dep0 : 0), (int32_t)(dep1 > dep0 ? dep1 : 0), 0});
+    ++piece;
+    if ((int64_t)steps.size() < most && piece < n_pieces) return ALORA_OK;
+    base = piece;
+    return launch();
+  });
+  if (st != ALORA_OK) return st;
   *done = true;
   return ALORA_OK;
 }

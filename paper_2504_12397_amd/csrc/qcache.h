@@ -52,6 +52,7 @@ struct RowsOrderedArgs {
 };
 constexpr int ROWS_TICKET_STRIDE = 32, ROWS_ORDERED_PLANES = 1024;
 constexpr int ROWS_ORDERED_UNITS = 256 * 8;      // most units that a piece of any plane has
+constexpr int ROWS_ORDERED_STEPS = 32768;        // most pieces of a launch (a table of 1.3 MB)
 void launch_rows_copy_ordered(const RowsOrderedArgs &a, const RowsFew &few, hipStream_t s);
 // T rows of n_kv heads of head_dim <-> rows of 4 bits; wide: head_dim is a multiple of 8, rows begin at multiples of 16 bytes, codes of 4
 template <typename T> void launch_rows_store(const RowsArgs &a, const RowsFew &few, int n_kv_heads, int head_dim, bool wide, hipStream_t s);
