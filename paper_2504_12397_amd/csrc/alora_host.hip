@@ -1665,15 +1665,22 @@ alora_status copy_rows(alora_ctx *ctx, const std::vector<CopyArray> &arrays, int
   std::vector<RowRange> out(job.ranges), back(job.ranges);
   int64_t at = 0;
   for (size_t i = 0; i < out.size(); ++i) { out[i].dst = at; back[i].src = at; at += out[i].n; }
-  for (size_t i = 0; i < arrays.size();) {
-    size_t j = i, bytes = 0;
-    for (; j < arrays.size(); ++j) {
-      const size_t b = ((size_t)job.rows * arrays[j].row_bytes + 255) & ~(size_t)255;
-      if (j > i && bytes + b > ((size_t)128 << 20)) break;
-      bytes += b;
-    }
-    st = ensure_workspace(ctx, bytes);
-    if (st != ALORA_OK) return st;
+  std::vector<size_t> ends;      // of the groups of arrays that are staged together
+  size_t largest = 0, bytes = 0;
+  for (size_t i = 0; i < arrays.size(); ++i) {
+    const size_t b = ((size_t)job.rows * arrays[i].row_bytes + 255) & ~(size_t)255;
+    if (bytes > 0 && bytes + b > ((size_t)128 << 20)) { ends.push_back(i); bytes = 0; }
+    bytes += b;
+    largest = std::max(largest, bytes);
+  }
+  ends.push_back(arrays.size());
+  // (all that has to be allocated is, before the first of them moves: a call that fails has moved nothing)
+  st = ensure_workspace(ctx, largest);
+  MetaSlot *grown = nullptr;
+  if (st == ALORA_OK) st = acquire_slot(ctx, job.ranges.size() * sizeof(RowRange) + arrays.size() * sizeof(RowPlane) + 32, &grown);
+  if (st != ALORA_OK) return st;
+  size_t i = 0;
+  for (size_t j : ends) {
     std::vector<RowPlane> to, from;
     Bump w(ctx->ws);
     for (; i < j; ++i) {

@@ -77,3 +77,19 @@ def test_time_on_the_host(ab, ctx, name):
     a, b = (full_caches(ab, 1, 2 * N + 10, 1, 2, "bf16", seed) for seed in (4, 5))
     apart, over = host(b, a), host(a, a)
     assert over <= 10 * apart, f"{1e3 * over:.2f} ms, between two pools {1e3 * apart:.2f}"
+
+
+def test_arrays_that_are_staged_in_groups_of_other_sizes(ab):
+    """Rows that change places, in arrays that go through a new context's workspace in groups, the second larger than the first."""
+    n = 100_000
+    ranges = [(0, n, n), (n, 0, n)]
+    ctx = ab.Context(0)
+    try:
+        c = four_caches(ab, 1, 2 * n, 8, 128, 6)
+        was = [t.clone() for t in arrays(c[0])]
+        ab.alora_qcache_copy(ctx, c, c, ranges)
+        torch.cuda.synchronize()
+        for t, w in zip(arrays(c[0]), was):
+            assert torch.equal(t[:n], w[n:]) and torch.equal(t[n:], w[:n])
+    finally:
+        ctx.close()
