@@ -183,6 +183,9 @@ const char *alora_status_string(alora_status s);
  *   "attn_partials16" 1 (default): when prefill attention is split over the keys, the partial results travel
  *                     as compact records (accumulators scaled to [-1, 1] as fp16 plus three fp32 scalars,
  *                     272 bytes).  0: fp32 records (520 bytes).
+ *   "qattn_fp16"      1 (default): attention over rows of 4 bits in bf16 with head size 64 or 128: (row, query head) pairs that
+ *                     read the same keys and are more than 16 multiply as fp16 where that holds the values -- one rounding of a probability to 11 bits.
+ *                     0: to 16 bits, as for fewer pairs and other head sizes; 128 rows of 32 heads on 32896 keys 138 us, so 117.
  *   "stage_copy"      0 (default): the per-call records (sequences, work lists) go from the pinned host ring to
  *                     device memory by a small kernel on the call's stream.  1: by hipMemcpyAsync.
  *   "profile"         0 (default) / 1: see alora_profile_read.
@@ -366,7 +369,7 @@ alora_status alora_qcache_load(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads
  *   cu_seqlens HOST [B+1] as in alora_prefill.  The S_b rows of sequence b are the last S_b of its seq_len[b] cached positions, all of them in its own
  *              rows (S_b <= seq_len[b] - prefix_len[b]): row i sees positions 0 .. seq_len[b] - S_b + i.  S_b = 0 leaves a sequence alone.
  *   out        DEVICE [T, n_q_heads * head_dim] (dtype), apart from q (ALORA_EINVAL where they overlap)
- * softmax(q k / sqrt(head_dim)) v with queries, keys and values as they are, sums in fp32; results of bf16 may come from probabilities of 11 bits (fp16).  A NaN in a key or value reaches the
+ * softmax(q k / sqrt(head_dim)) v with queries, keys and values as they are, sums in fp32; results of bf16 may come from probabilities of 11 bits (see "qattn_fp16").  A NaN in a key or value reaches the
  * rows that see its position and no others.  Sequences of the call may name the same rows.  Prefixes that several sequences name are walked once for all of
  * them.  Errors as everywhere; under capture into a HIP graph ALORA_EINVAL (the call stages its work list from the host). */
 alora_status alora_qcache_attend(alora_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *cache,

@@ -117,6 +117,7 @@ struct alora_ctx {
   int opt_attn_partials16 = 1;   // split prefill attention (MFMA path): compact partial records
   int opt_rope_fuse = 1;         // rotation + cache append in the epilogue of the QKV projection where the shape allows
   int opt_attn_fold = 1;         // 1 = prefill attention takes prescaled queries and starts its score accumulators at -m_ref
+  int opt_qattn_fp16 = 1;        // attention over rows of 4 bits: units of many columns multiply in fp16 where it holds the values
   int n_cu = 256;
 };
 
@@ -1958,7 +1959,7 @@ void run_qattn(alora_ctx *ctx, const QAttnPlan &q, const char *staged, const Lay
         a.hw = c.hw; a.kr = c.kr; a.cw = c.cw;
         const int ht = qattn_ht(L.head_dim);
         // (fp16, and what was too narrow for it)
-        const bool half = q.lds && c.nc > 1 && qt != Q_F32;
+        const bool half = ctx->opt_qattn_fp16 && q.lds && c.nc > 1 && qt != Q_F32;
         a.narrow = half ? narrow : nullptr;
         for (int pass = half ? 0 : 1; pass < 2; ++pass) {
           if (qt == Q_BF16) launch_qattn_mfma_bf16(a, n, ht, c.nc, q.lds, pass == 0, s);
@@ -2599,6 +2600,11 @@ alora_status alora_set_option(alora_ctx *ctx, const char *key, int value) {
   if (!strcmp(key, "gemm_tile")) {
     if (value < 0 || value > 6) return fail(ctx, ALORA_EINVAL, "gemm_tile must be in [0, 6]");
     ctx->opt_gemm_tile = value;
+    return ALORA_OK;
+  }
+  if (!strcmp(key, "qattn_fp16")) {
+    if (value != 0 && value != 1) return fail(ctx, ALORA_EINVAL, "qattn_fp16 must be 0 or 1");
+    ctx->opt_qattn_fp16 = value;
     return ALORA_OK;
   }
   if (!strcmp(key, "profile")) {

@@ -221,3 +221,8 @@ def test_more_pieces_than_a_launch_takes(ab, v, call):
         st = {"cache_copy": lambda: lib.alora_cache_copy(v, 1, 1, 2, C.byref(b), C.byref(a), 1, p, m, None),
               "qcache_store": lambda: lib.alora_qcache_store(v, 1, 1, 2, C.byref(c), C.byref(a), 1, p, m, None)}[call]()
         assert status(ab, st) == want
+
+
+def test_option_of_attention_over_rows_of_4_bits(ab, v):
+    for value, want in ((0, ab.ALORA_OK), (1, ab.ALORA_OK), (2, ab.ALORA_EINVAL), (-1, ab.ALORA_EINVAL)):
+        assert ab._lib.alora_set_option(v, b"qattn_fp16", value) == want

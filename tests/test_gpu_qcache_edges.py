@@ -256,3 +256,38 @@ def test_stacks_layer_by_layer(ab, ctx, name, decode):
         x = y
     H.report(check="qcache stack", err=worst, tol=tol)
     assert torch.equal(out, x)
+
+
+@pytest.mark.parametrize("h", [64, 128])
+def test_option_for_probabilities_of_16_bits(ab, h):
+    """qattn_fp16 = 0: a probability is rounded to 16 bits, one of 11 bits is 2^5 times as far off.  A result is stored as another number than the one next to the exact
+    value where the exact value lies nearer to the middle between two numbers than the error: in proportion to the error, so in far fewer places (fp32 sums add some to both)."""
+    c = ab.Context(0)
+    try:
+        b = Batch(ab, "bf16", 8, 2, h, [900, 300], [60, 9], C=[500], group=[0, 0], seed=47)
+        off = {}
+        for value in (1, 0):
+            c.set_option("qattn_fp16", value)
+            out = ab.alora_qcache_attend(c, b.cache, b.q, b.cu, 8)
+            b.check(out)
+            want = torch.cat([torch.from_numpy(b.reference(i)[0]) for i in range(2)]).to(torch.bfloat16)
+            off[value] = float((out.cpu() != want).double().mean())
+        H.report(check="qattn_fp16", off_11_bits=off[1], off_16_bits=off[0])
+        assert off[0] < off[1] / 4
+        # a value that is not a number, and values that fp16 does not hold, on this path alone
+        codes, e = b.codes[1]
+        e[b.rows(0)[-20], 0, 1] = 255
+        nan = torch.isnan(ab.alora_qcache_attend(c, b.make(ab), b.q, b.cu, 8)).cpu().view(69, 8, h)
+        want = torch.zeros_like(nan)
+        want[40:60, :4, 32:64] = True
+        assert torch.equal(nan, want)
+        e[b.rows(0)[-20], 0, 1] = 160
+        b.cache = b.make(ab)
+        b.check(ab.alora_qcache_attend(c, b.cache, b.q, b.cu, 8))
+        case = H.make_case(LAYER["bf16"], [200, 40], [40, 33], [200, 40], [0, 1], seed=48, prefix="random")
+        full = H.gpu_cache(case)
+        four = q_copy(ab, c, full)
+        out = ab.alora_qcache_prefill(c, H.gpu_layer(case, LAYER["bf16"]), four, case.x_packed.cuda().contiguous(), case.cu, case.k, case.adapter)
+        check_layers(ab, c, case, four, full, out, False)
+    finally:
+        c.close()
