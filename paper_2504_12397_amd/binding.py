@@ -158,10 +158,18 @@ class Layer:
         self.d = int(W.shape[1])
         self.dtype = W.dtype
         self.device = W.device
+        self.on = W.get_device()
 
 
 def _table(x, dtype):
     return None if x is None else np.ascontiguousarray(np.asarray(x, dtype=dtype))
+
+
+def _one_device(*arrays) -> int:
+    on = arrays[0].get_device()
+    if any([a.get_device() != on for a in arrays]):
+        raise ValueError(f"arrays of one cache on {[str(a.device) for a in arrays]}")
+    return on
 
 
 class _Pool:
@@ -250,7 +258,7 @@ class KVCache(_Pool):
 
     def _refresh(self):
         self.desc = KVCacheDesc(_ptr(self.k), _ptr(self.v), self.pool_tokens, *self._tables())
-        self.kind = (int(self.k.shape[1]), self.head_dim, self.k.dtype)
+        self.kind = (int(self.k.shape[1]), self.head_dim, self.k.dtype, _one_device(self.k, self.v))
 
     def rows(self, b: int, lo: int, hi: int):
         o = int(self.seq_offset[b])
@@ -292,7 +300,7 @@ class QCache(_Pool):
 
     def _refresh(self):
         self.desc = QCacheDesc(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), self.pool_tokens, *self._tables())
-        self.kind = (int(self.k.shape[1]), self.head_dim, self.k.dtype)
+        self.kind = (int(self.k.shape[1]), self.head_dim, self.k.dtype, _one_device(self.k, self.v, self.k_scale, self.v_scale))
 
 
 class Context:
@@ -466,14 +474,27 @@ def _address(a: np.ndarray) -> int:
     return a.__array_interface__["data"][0]
 
 
+def _reach(ctx: Context, on: Sequence[int], tensors):
+    """The GPU of the context reaches what is on these devices (-1: the host, where it reaches pinned memory); tensors() lists it all."""
+    if ctx.device >= 0 and any([n != ctx.device for n in on]):
+        for t in tensors():
+            if t is not None and t.get_device() != ctx.device and not (t.get_device() < 0 and t.is_pinned()):
+                raise ValueError(f"a tensor on {t.device}, which the context's GPU {ctx.device} does not reach")
+
+
+def _arrays(c: _Pool):
+    return [c.k, c.v] + ([c.k_scale, c.v_scale] if isinstance(c, QCache) else [])
+
+
 def _move(name: str, ctx: Context, dst, src, ranges, stream, typed=None):
     """The four calls that move rows: caches are one, or a list of them, one per layer; typed: the side whose type the call is told."""
     d, s = ([dst] if isinstance(dst, _Pool) else dst), ([src] if isinstance(src, _Pool) else src)
     if len(d) != len(s) or len(d) == 0:
         raise ValueError(f"{len(d)} destination and {len(s)} source layers")
     to, of = d[0].kind, s[0].kind
-    if any([c.kind != to for c in d]) or any([c.kind != of for c in s]) or to[:2] != of[:2] or (typed is None and to != of):
+    if any([c.kind != to for c in d]) or any([c.kind != of for c in s]) or to[:2] != of[:2] or (typed is None and to[2] != of[2]):
         raise ValueError(f"caches of different shapes or types: {[c.kind for c in d]} and {[c.kind for c in s]}")
+    _reach(ctx, (to[3], of[3]), lambda: [t for c in (*d, *s) for t in _arrays(c)])
     r = np.ascontiguousarray(np.asarray(ranges, dtype=np.int64).reshape(-1, 3))
     kind = () if name == "alora_qcache_copy" else (_DTYPES[(to if typed == "dst" else of)[2]],)
     ctx._check(getattr(_lib, name)(ctx._h, *kind, *to[:2], b"".join([bytes(c.desc) for c in d]), b"".join([bytes(c.desc) for c in s]), len(d),
@@ -512,6 +533,7 @@ def alora_qcache_attend(ctx: Context, cache: QCache, q: torch.Tensor, cu_seqlens
         raise ValueError(f"q {tuple(q.shape)} and out {tuple(out.shape)} have to be [{int(cu[-1])}, {n_q_heads * h}], fp32 or bf16")
     if not cache._holds(len(cu) - 1):
         raise ValueError(f"{len(cu) - 1} sequences are more than the tables of the cache hold")
+    _reach(ctx, (cache.kind[3], q.get_device(), out.get_device()), lambda: [*_arrays(cache), q, out])
     ctx._check(_lib.alora_qcache_attend(ctx._h, _DTYPES[q.dtype], n_q_heads, int(cache.k.shape[1]), h, C.byref(cache.desc), _ptr(q), _address(cu),
                                         len(cu) - 1, _ptr(out), _stream_ptr(stream)))
     return out
@@ -531,6 +553,8 @@ def _q_call(name, ctx, layers, caches, x, cu, k_per_seq, adapter_per_seq, out, w
         raise ValueError(f"x {tuple(x.shape)} has to be [{T}, {layers[0].d}] and out [{T}, {width}], both of the layers' type")
     if out is None:
         out = torch.empty((x.shape[0], width), dtype=layers[0].dtype, device=layers[0].device)
+    _reach(ctx, (x.get_device(), out.get_device(), *[c.kind[3] for c in caches], *[l.on for l in layers]),
+           lambda: [x, out] + [t for c in caches for t in _arrays(c)] + [l.t["W_qkv"] for l in layers])
     p = C.POINTER(C.c_int32)
     descs = b"".join([bytes(c.desc) for c in caches])
     args = [ctx._h, (LayerDesc * len(layers))(*[l.desc for l in layers])] + ([len(layers)] if stack else []) + [descs, _ptr(x)]
