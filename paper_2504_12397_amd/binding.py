@@ -193,9 +193,10 @@ class _Pool:
         self.seq_offset, self.seq_capacity = _table(seq_offset, np.int64), _table(seq_capacity, np.int32)
         self.seq_len = _table(seq_len, np.int32)
         self.prefix_offset, self.prefix_len = _table(prefix_offset, np.int64), _table(prefix_len, np.int32)
-        own, shared = (self.seq_offset, self.seq_capacity, self.seq_len), (self.prefix_offset, self.prefix_len)
-        if len({len(t) for t in own + (shared if shared[1] is not None else ()) if t is not None}) > 1 or (shared[1] is not None and shared[0] is None):
-            raise ValueError(f"tables of {[None if t is None else len(t) for t in own + shared]} sequences")
+        tables = [self.seq_offset, self.seq_capacity, self.seq_len] + ([] if self.prefix_len is None else [self.prefix_offset, self.prefix_len])
+        lengths = [len(t) for t in tables if t is not None]
+        if lengths and (lengths != lengths[:1] * len(lengths) or (self.prefix_len is not None and self.prefix_offset is None)):
+            raise ValueError(f"tables of {[None if t is None else len(t) for t in tables]} sequences")
         self._refresh()
         return self
 
