@@ -320,7 +320,8 @@ alora_status alora_lm_head(alora_ctx *ctx, alora_dtype dtype, int32_t d, int32_t
  * Format.  Row (token, kv head) has head_dim codes of 4 bits: a sign (bit 3) and a magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits
  * 2..0 = 0..7); element 2i is in the low half of byte i.  Each 32 channels of a head (the last block may be shorter) share one
  * exponent byte E: value = code * 2^(E - 127).  Storing takes E - 127 = e - 2 from the block's largest magnitude m * 2^e, 1 <= m < 2, or
- * e - 1 where m > 1.75 (at most a seventh of that magnitude is cut off), kept between -125 and 125, 0 for a block of zeros, and rounds every channel to the
+ * e - 1 where m > 1.75 (at most a seventh of that magnitude is cut off), kept between -125 and 125 (a magnitude over 1.75 * 2^127 loses up to a
+ * quarter), 0 for a block of zeros, and rounds every channel to the
  * nearest code, ties to the even one, magnitudes over 6 to 6.  Scales are powers of two, so a code depends on nothing but its
  * block's bits, and loading is exact in bf16 and fp32.  A block that holds a NaN or an infinity gets E = 255: all its values are NaN.
  * Other E outside [2, 252] are never stored; what attention makes of them is undefined. */
@@ -369,7 +370,7 @@ alora_status alora_qcache_load(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads
  *   cu_seqlens HOST [B+1] as in alora_prefill.  The S_b rows of sequence b are the last S_b of its seq_len[b] cached positions, all of them in its own
  *              rows (S_b <= seq_len[b] - prefix_len[b]): row i sees positions 0 .. seq_len[b] - S_b + i.  S_b = 0 leaves a sequence alone.
  *   out        DEVICE [T, n_q_heads * head_dim] (dtype), apart from q (ALORA_EINVAL where they overlap)
- * softmax(q k / sqrt(head_dim)) v with queries, keys and values as they are, sums in fp32; results of bf16 may come from probabilities of 11 bits (see "qattn_fp16").  A NaN in a key or value reaches the
+ * softmax(q k / sqrt(head_dim)) v with queries, keys and values as they are, sums in fp32 before they are divided (values near 3e38 overflow them, as elsewhere); results of bf16 may come from probabilities of 11 bits (see "qattn_fp16").  A NaN in a key or value reaches the
  * rows that see its position and no others.  Sequences of the call may name the same rows.  Prefixes that several sequences name are walked once for all of
  * them.  Errors as everywhere; under capture into a HIP graph ALORA_EINVAL (the call stages its work list from the host). */
 alora_status alora_qcache_attend(alora_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *cache,

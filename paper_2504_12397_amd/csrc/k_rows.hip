@@ -105,7 +105,7 @@ void launch_rows_copy_ordered(const RowsOrderedArgs &a, const RowsFew &few, hipS
 
 // ---- rows of the storage type <-> rows of 4 bits -------------------------------------------------------------
 // The exponent byte of a block with this largest magnitude (as bits): that of the magnitude less 2, so that it lands in [4, 8) of the
-// codes' [0, 6]; less 1 where its mantissa is over 1.75, so that at most a seventh of the magnitude is cut off (7 -> 6).  Blocks of zeros have 127.
+// codes' [0, 6]; less 1 where its mantissa is over 1.75, so that at most a seventh of the magnitude is cut off (7 -> 6; at Q_E_MAX, over 1.75 * 2^127, 8 -> 6).  Blocks of zeros have 127.
 __device__ __forceinline__ int q_exponent(uint32_t amax_bits) {
   if (amax_bits >= 0x7f800000u) return Q_E_NAN;
   const int e = (int)((amax_bits + 0x1fffffu) >> 23) - 2;

@@ -1,7 +1,7 @@
 // Attention over rows of 4 bits on the matrix units (Eq.1 with the causal mask, Eq.4): for head sizes that are multiples of 8.
 //
 // A wave takes 16 * NC columns -- (row, query head) pairs that read one kv head -- and walks a range of keys, 32 a step:
-//   * Codes of K go from memory straight into the A operand of v_mfma_f32_16x16x32_bf16: lane (j, kg) has the HT / 4 channels from kg * HT / 4 on of
+//   * Codes of K go, as they are, into the A operand of v_mfma_f32_16x16x32_bf16: lane (j, kg) has the HT / 4 channels from kg * HT / 4 on of
 //     key j of 16, a dword (8 channels) per product; the queries, laid out alike, are the B operand: S[key][column].  v_cvt_scalef32_pk_bf16_fp4
 //     turns two codes into two numbers, scale included, in one instruction: bf16 holds every code times every power of two exactly, where
 //     fp16 would overflow or lose bits for exponents far from 127.
@@ -9,14 +9,16 @@
 //     for a new maximum, and the probabilities of two blocks of 16 keys are, as they sit, the B operand (32 keys) of O += V P.
 //   * V: lane (j, kg) has CPL = HT / 16 channels from CPL j on of those 8 keys; after conversion a byte permute of two keys' words puts
 //     one channel of two keys side by side, which is the transposition: product c is channel CPL i + c of lane row i.
-// No LDS and no barrier but where several waves share a head's keys (KR > 1): they join at the end, in pairs.
+// Two kernels differ in how codes reach the lanes' registers: through LDS (heads of 64 and 128: qattn_lds_kernel), or from memory (qattn_mfma_kernel: any head size and alignment).  Where
+// several waves share a head's keys (KR > 1), they join through LDS at the end, in pairs.
 // Queries of bf16 are one operand, exactly; fp16 two (high and low bits as bf16; one beside keys of fp16, below), fp32 three.  Probabilities are two operands (16 bits; one of 8
 // bits would add half of what the rounding of a bf16 result does), three for fp32.  Units of many columns, where the products count and not memory, take one operand
 // of fp16 (11 bits) with values of fp16, as long as that holds them exactly: a workgroup looks at the smallest exponent that it met and at whether its sums
 // are numbers (queries of fp16 take keys of fp16 likewise: both ends of their exponents count), and says so where fp16 was too narrow; a second launch does those items, and no others, with operands of bf16.  128 rows of 32 heads on 32896 keys
 // 139 -> 117 us, the second launch (4 us) included.
 // The reference exponent of a column moves only when a score exceeds it by 2^8 more than it did: almost no step rescales the sums.  It begins 8 above the largest score
-// so far, so that probabilities are 1 at most (values may be as large as fp32 holds); in fp16 7 below it, for the sake of that type's small numbers: 2^15 at most.
+// so far, so that probabilities are 1 at most and 2^-8 at a new maximum (sums of values near fp32's largest have that much room: about 300 keys of equal weight); in fp16 7 below it, for the sake
+// of that type's small numbers: 2^15 at most.
 #pragma once
 #include "lds_dma.h"
 #include "qcache.h"
