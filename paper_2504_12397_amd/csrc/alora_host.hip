@@ -1885,7 +1885,8 @@ QAttnPlan plan_qattn(const alora_ctx *ctx, const Plan &pl, const LayerDims &L, Q
         if (parts == 1 || cost < best) { best = cost; r = len; }
       }
     }
-    // (one row on 131072 keys: 256 records a head are merged in 9 us; half as many, with two waves on every head's keys, 46.9 -> 43.5 us, a quarter 45.5)
+    // More than 128 records a head take long to merge: half as many, with two waves on every head's keys.  One row, 8 kv heads of 128: 17000 keys 21.4 us, so 19.9; 32768 26.1, 22.7; 131071
+    // 40.3, 38.2; 262144 60.9 both (heads of 64: 19.7, 18.0; 22.8, 19.5; 34.2, 31.0; 49.2, 45.5).  With 16 kv heads and more a range is never cut so finely.
     if (ctx->opt_splits == 0 && c.kr == 1 && c.hw == 8 && longest > 128 * r) { c.hw = 4; c.kr = 2; r *= 2; }
     r = std::min((r + 31) & ~(int64_t)31, (longest + 31) & ~(int64_t)31);
     range[k] = (int)r;
