@@ -347,7 +347,7 @@ typedef struct { int64_t src, dst, n; } alora_row_range;
  * arrays).  The bookkeeping -- whose rows they are now -- is the caller's: only k, v and pool_tokens of the caches are read.
  *   dst, src  HOST [n_layers]: caches of one shape (dtype, n_kv_heads, head_dim); pools may differ in size, each is the same in all layers
  *   ranges    HOST [n_ranges]; rows outside a pool: ALORA_ECAPACITY; destination ranges that overlap each other, negative n: ALORA_EINVAL.
- *             n = 0 is allowed, and n_ranges = 0 is a valid no-op.
+ *             n = 0 is allowed, and n_ranges = 0 is a valid no-op.  Ranges travel in pieces (32 KB of rows, or a range that is shorter); 2^24 of them: ALORA_EINVAL.
  * dst[l] and src[l] are the same arrays or do not overlap in memory (ALORA_EINVAL where bases differ and memory overlaps); arrays of different layers, and
  * keys and values, never overlap.  Rows that move
  * over others, some towards the front and some towards the back, are staged through the context's workspace. */
@@ -372,7 +372,9 @@ alora_status alora_qcache_load(alora_ctx *ctx, int32_t dtype, int32_t n_kv_heads
  *   out        DEVICE [T, n_q_heads * head_dim] (dtype), apart from q (ALORA_EINVAL where they overlap)
  * softmax(q k / sqrt(head_dim)) v with queries, keys and values as they are, sums in fp32 before they are divided (values near 3e38 overflow them, as elsewhere); results of bf16 may come from probabilities of 11 bits (see "qattn_fp16").  A NaN in a key or value reaches the
  * rows that see its position and no others.  Sequences of the call may name the same rows.  Prefixes that several sequences name are walked once for all of
- * them.  Errors as everywhere; under capture into a HIP graph ALORA_EINVAL (the call stages its work list from the host). */
+ * them.  Errors as everywhere; ALORA_EINVAL also for rows times heads beyond 2^30, or beyond 2^26 where a
+ * (row, head) is a wave of its own (head sizes that are no multiple of 8, codes or queries that are not aligned, results joined from parts), and under capture into a HIP graph
+ * (the call stages its work list from the host). */
 alora_status alora_qcache_attend(alora_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const alora_qcache *cache,
                                  const void *q, const int32_t *cu_seqlens, int32_t B, void *out, void *stream);
 
